@@ -40,7 +40,7 @@ typedef enum {
     TA_ERR_NULL_POINTER = 1,  /* a required pointer is NULL                                 */
     TA_ERR_INVALID_SHAPE = 2, /* a size < 1, Hq % Hkv != 0, causal with Sq > Sk, or an
                                  element count beyond 2^31 per (batch, head) slice         */
-    TA_ERR_UNSUPPORTED = 3,   /* D is not 64 or 128                                         */
+    TA_ERR_UNSUPPORTED = 3,   /* D is not 64 or 128, or another value that is not offered   */
     TA_ERR_MISALIGNED = 4,    /* a pointer is not 16-byte aligned                           */
     TA_ERR_INVALID_SCALE = 5, /* scale is negative, NaN or infinite                         */
     TA_ERR_ALIASING = 6,      /* O or LSE overlaps an input or each other                   */
@@ -401,6 +401,116 @@ ta_status ssd_forward_workspace_bytes(int batch, int seqlen, int nheads, int num
 
 /* A segment count for ssd_forward.  No HIP call. */
 ta_status ssd_segment_heuristic(int batch, int seqlen, int nheads, int *num_segments);
+
+/*
+ * Paged key/value cache of a decoder's serving step.  K and V of all sequences
+ * live in one pool of pages each; a page holds page_size consecutive positions
+ * of one sequence, and row b of page_table names the pages of sequence b in
+ * order, so that position t of it is row t % page_size of page
+ * page_table[b][t / page_size].
+ *
+ *   K_cache, V_cache  device, [num_pages, Hkv, page_size, D], bf16, or 8-bit
+ *                     (OCP e4m3) if cache_e4m3 != 0
+ *   k_scale, v_scale  device, fp32 [Hkv], or NULL for 1: an 8-bit number c of
+ *                     head h stands for c * scale[h].  NULL for a bf16 cache
+ *                     (else TA_ERR_UNSUPPORTED)
+ *   page_table        device, int32 [B, max_pages]
+ *   D in {64, 128}; page_size a power of two, at least 16 (else
+ *   TA_ERR_UNSUPPORTED); max_pages * page_size <= 2^30 and num_pages <= 2^28
+ *   (else TA_ERR_INVALID_SHAPE).  Caches 16-byte aligned, fp32 and int32
+ *   vectors 4-byte aligned.
+ * What the arrays on the device hold cannot be checked before the launch; the
+ * kernels check every index they take from them, and address nothing outside
+ * the caches whatever they hold.
+ */
+
+/*
+ * kv_cache_append — writes new tokens' keys and values into the paged cache.
+ *
+ *   K, V      device, bf16 [T, Hkv, D], read only: token t starts k_stride
+ *             (v_stride) elements after token t - 1 (at least Hkv * D, a
+ *             multiple of 8), so that they can be slices of a fused
+ *             projection; 16-byte aligned
+ *   seq       device, int32 [T]: token t belongs to sequence seq[t]; NULL:
+ *             token t belongs to sequence t (T <= B, else TA_ERR_INVALID_SHAPE)
+ *   pos       device, int32 [T]: its position in that sequence.  A token whose
+ *             position is negative (padding) or past the table, whose seq is
+ *             not in 0..B-1 or whose page is not in 0..num_pages-1 is left out
+ *   K_cache, V_cache  written at those positions only
+ *
+ * An 8-bit cache takes x / scale rounded to the nearest e4m3 number (to even),
+ * beyond +-448 as +-448, infinities too; NaN stays NaN.  Of two tokens of one
+ * call with the same place, which one it holds afterwards is not defined, piece
+ * of 16 bytes by piece.  Caches must not overlap each other or an input
+ * (TA_ERR_ALIASING).  Ownership, asynchrony and status codes as attn_fwd.
+ */
+ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_t v_stride,
+                          const int *seq, const int *pos, void *K_cache, void *V_cache,
+                          int cache_e4m3, const float *k_scale, const float *v_scale,
+                          const int *page_table, int T, int B, int Hkv, int D, int num_pages,
+                          int page_size, int max_pages, void *stream);
+
+/*
+ * attn_decode_paged — attention of one new token per sequence over the paged
+ * cache: for sequence b of seq_lens[b] positions, query head h and key/value
+ * head hk = h / (Hq / Hkv),
+ *   s_t = scale * Q[b,h,:] . K_t,  O[b,h,:] = sum_t softmax(s)_t V_t,
+ *   LSE[b,h] = ln sum_t exp(s_t)
+ * over its positions t (the new token's own included, once appended).
+ *
+ *   Q         device, bf16 [B, Hq, D], read only: sequence b starts q_stride
+ *             elements after sequence b - 1 (at least Hq * D, a multiple of 8);
+ *             16-byte aligned
+ *   seq_lens  device, int32 [B], from 0 to max_pages * page_size.  Length 0 (an
+ *             idle slot of a padded batch) gives O = 0 and LSE = -inf.  Any other
+ *             value outside, and a page outside 0..num_pages-1 among those of
+ *             the sequence's positions, gives NaN in that sequence's O and LSE
+ *   O         device, [B, Hq, D]: fp32, or bf16 if o_bf16 != 0      written
+ *   LSE       device, fp32 [B, Hq]                                  written
+ *   Hq % Hkv == 0; scale >= 0, finite; O and LSE 16-byte aligned and apart
+ *   from each other and from every input (TA_ERR_ALIASING)
+ *
+ * Entries of page_table past a sequence's last page, and what the caches hold
+ * past its last position, are never used.  Scores and sums are fp32; the softmax
+ * weights enter the product with V as two bf16 numbers each (16 bits), three (24
+ * bits) for an fp32 O.  Ownership, asynchrony and status codes as attn_fwd.
+ */
+ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache,
+                            const void *V_cache, int cache_e4m3, const float *k_scale,
+                            const float *v_scale, const int *page_table, const int *seq_lens,
+                            void *O, int o_bf16, float *LSE, int B, int Hq, int Hkv, int D,
+                            int num_pages, int page_size, int max_pages, float scale,
+                            void *stream);
+
+/* Activations of gemm_bf16_epilogue */
+typedef enum {
+    TA_ACT_NONE = 0,
+    TA_ACT_RELU = 1,      /* max(x, 0)                                                    */
+    TA_ACT_GELU = 2,      /* x (1 + erf(x / sqrt 2)) / 2                                  */
+    TA_ACT_GELU_TANH = 3, /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2            */
+    TA_ACT_SILU = 4       /* x / (1 + exp(-x))                                            */
+} ta_activation;
+
+/*
+ * gemm_bf16_epilogue — C = act(A B + bias) + residual, for any number of rows.
+ *
+ *   A  device, bf16 [M, K] row-major             read only
+ *   B  device, bf16 [K, N] row-major             read only
+ *   bias      device, bf16 [N], or NULL          read only
+ *   residual  device, [M, N] row-major, of C's type, or NULL; may be C itself
+ *             (the sum in place), otherwise read only
+ *   C  device, [M, N] row-major: fp32, or bf16 if c_bf16 != 0      written
+ *   activation  a ta_activation (else TA_ERR_UNSUPPORTED)
+ *   N % 8 == 0 and K % 8 == 0 (else TA_ERR_UNSUPPORTED); N < 2^24, K < 2^22,
+ *   M * N < 2^40 and M * K < 2^40 (else TA_ERR_INVALID_SHAPE); pointers 16-byte
+ *   aligned; C apart from A, B and bias, and from residual unless it is C
+ *
+ * Sums, bias, activation and residual are fp32; a bf16 C is rounded once, to
+ * nearest even.  Ownership, asynchrony and status codes as gemm_bf16.
+ */
+ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, const void *residual,
+                             void *C, int c_bf16, int activation, int M, int N, int K,
+                             void *stream);
 
 /*
  * ta_schedule — host-side tile schedule of attn_fwd, for tests and tools.

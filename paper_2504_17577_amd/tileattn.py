@@ -104,6 +104,12 @@ def lib():
     L.ssd_forward_workspace_bytes.argtypes = [i] * 4 + [ctypes.POINTER(ctypes.c_size_t)]
     L.ssd_segment_heuristic.restype = i
     L.ssd_segment_heuristic.argtypes = [i] * 3 + [ctypes.POINTER(i)]
+    L.kv_cache_append.restype = i
+    L.kv_cache_append.argtypes = [p, p, ctypes.c_int64, ctypes.c_int64, p, p, p, p, i, p, p, p] + [i] * 7 + [p]
+    L.attn_decode_paged.restype = i
+    L.attn_decode_paged.argtypes = [p, ctypes.c_int64, p, p, i, p, p, p, p, p, i, p] + [i] * 7 + [ctypes.c_float, p]
+    L.gemm_bf16_epilogue.restype = i
+    L.gemm_bf16_epilogue.argtypes = [p] * 5 + [i] * 5 + [p]
     L.ta_schedule.restype = i
     L.ta_schedule.argtypes = [i, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
     L.ta_tile_shape.restype = i
@@ -698,3 +704,141 @@ def ssd_forward(x, dt, A, Bm, Cm, D=None, stream=None, num_segments: int | None 
                                      num_segments, ws.data_ptr() if need else None, need,
                                      _stream_handle(stream or None, x)))
     return out, final
+
+
+# ---------------------------------------------------------------------------
+# A decoder's serving step: paged cache (include/tileattn.h documents the
+# layout in full) and the matrix product with its epilogue.
+
+def _rows(name, t, shape):
+    """The element stride between the first-dimension rows of a bf16 GPU tensor of
+    this shape whose rows are contiguous (a slice of a wider tensor's columns)."""
+    if t.dtype != torch.bfloat16 or not t.is_cuda or tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{name} must be a bfloat16 GPU tensor of shape {tuple(shape)}")
+    n, h, d = shape
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+        raise TypeError(f"{name}: each [{h}, {d}] row must be contiguous")
+    return t.stride(0) if n > 1 else h * d
+
+
+def _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table):
+    """(Hkv, D, num_pages, page_size, B, max_pages, e4m3) of a paged cache, checked."""
+    e4m3 = k_cache.dtype == torch.float8_e4m3fn
+    if k_cache.dim() != 4 or not (e4m3 or k_cache.dtype == torch.bfloat16):
+        raise TypeError("k_cache must be a 4-D bfloat16 or float8_e4m3fn tensor [num_pages, Hkv, page_size, D]")
+    num_pages, Hkv, page_size, D = k_cache.shape
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if t.dtype != k_cache.dtype or not t.is_cuda or tuple(t.shape) != tuple(k_cache.shape) or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous {k_cache.dtype} GPU tensor of shape {tuple(k_cache.shape)}")
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if t is not None:
+            if not e4m3:
+                raise TileAttnError(3, f"{name} goes with a float8_e4m3fn cache")
+            _vector(name, t, torch.float32, (Hkv,))
+    if page_table.dim() != 2:
+        raise TypeError("page_table must be 2-D [B, max_pages]")
+    B, max_pages = page_table.shape
+    _vector("page_table", page_table, torch.int32, (B, max_pages))
+    return Hkv, D, num_pages, page_size, B, max_pages, e4m3
+
+
+def _vector(name, t, dtype, shape):
+    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def kv_cache_append(k, v, k_cache, v_cache, page_table, pos, seq=None, k_scale=None, v_scale=None,
+                    stream=None):
+    """Writes new tokens' k, v [T, Hkv, D] (bf16; slices of a fused projection
+    will do) into the paged caches [num_pages, Hkv, page_size, D] (bf16 or
+    float8_e4m3fn) at positions pos [T] of sequences seq [T] (default: token t of
+    sequence t); page_table [B, max_pages], pos and seq are int32 GPU tensors, the
+    scales fp32 [Hkv] (default 1).  Tokens with a negative position are left out.
+    Returns (k_cache, v_cache)."""
+    Hkv, D, num_pages, page_size, B, max_pages, e4m3 = _paged_cache(k_cache, v_cache, k_scale, v_scale,
+                                                                    page_table)
+    T = k.shape[0]
+    ks, vs = _rows("k", k, (T, Hkv, D)), _rows("v", v, (T, Hkv, D))
+    _vector("pos", pos, torch.int32, (T,))
+    if seq is not None:
+        _vector("seq", seq, torch.int32, (T,))
+    with _one_device(k, v, k_cache, v_cache, page_table, pos, seq, k_scale, v_scale):
+        rc = lib().kv_cache_append(k.data_ptr(), v.data_ptr(), ks, vs, _ptr(seq), pos.data_ptr(),
+                                   k_cache.data_ptr(), v_cache.data_ptr(), int(e4m3), _ptr(k_scale),
+                                   _ptr(v_scale), page_table.data_ptr(), T, B, Hkv, D, num_pages,
+                                   page_size, max_pages, _stream_handle(stream, k))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return k_cache, v_cache
+
+
+def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | None = None,
+                      k_scale=None, v_scale=None, out=None, lse=None, out_dtype=None, stream=None):
+    """O [B, Hq, D], LSE [B, Hq] (fp32) = attention of one new token per sequence,
+    q [B, Hq, D] bf16 (a slice of a fused projection will do), over the first
+    seq_lens[b] (int32 GPU tensor [B]) positions of its pages; caches, table and
+    scales as kv_cache_append takes them.  ``scale`` defaults to 1/sqrt(D),
+    ``out_dtype`` is torch.float32 (default) or torch.bfloat16.  A sequence of
+    length 0 gets O = 0 and LSE = -inf."""
+    o_dtype = torch.float32 if out_dtype is None else out_dtype
+    if o_dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
+    Hkv, D, num_pages, page_size, B, max_pages, e4m3 = _paged_cache(k_cache, v_cache, k_scale, v_scale,
+                                                                    page_table)
+    if q.dim() != 3:
+        raise TypeError("q must be a 3-D bfloat16 GPU tensor [B, Hq, D]")
+    Hq = q.shape[1]
+    q_stride = _rows("q", q, (B, Hq, D))
+    _vector("seq_lens", seq_lens, torch.int32, (B,))
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    out = _output("out", out, (B, Hq, D), o_dtype, q)
+    lse = _output("lse", lse, (B, Hq), torch.float32, q)
+    with _one_device(q, k_cache, v_cache, page_table, seq_lens, k_scale, v_scale, out, lse):
+        rc = lib().attn_decode_paged(q.data_ptr(), q_stride, k_cache.data_ptr(), v_cache.data_ptr(),
+                                     int(e4m3), _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(),
+                                     seq_lens.data_ptr(), out.data_ptr(), int(o_dtype == torch.bfloat16),
+                                     lse.data_ptr(), B, Hq, Hkv, D, num_pages, page_size, max_pages,
+                                     float(scale), _stream_handle(stream, q))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return out, lse
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None, out=None,
+                       out_dtype=None, stream=None):
+    """C = act(A B + bias) + residual for contiguous bfloat16 GPU matrices a [M, K]
+    (any M) and b [K, N] (N and K multiples of 8), bias [N] bf16; C and residual
+    [M, N] are float32 (default) or bfloat16 (``out_dtype``).  ``activation``:
+    none, relu, gelu (by erf), gelu_tanh or silu.  ``out`` may be ``residual``."""
+    for name, t in (("a", a), ("b", b)):
+        if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 2 or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous 2-D bfloat16 GPU tensor")
+    M, K = a.shape
+    K2, N = b.shape
+    if K2 != K:
+        raise TileAttnError(2, f"inconsistent shapes a{tuple(a.shape)} b{tuple(b.shape)}")
+    if activation not in ACTIVATIONS:
+        raise TileAttnError(3, f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
+    dt = torch.float32 if out_dtype is None else out_dtype
+    if dt not in (torch.float32, torch.bfloat16):
+        raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
+    if bias is not None:
+        _vector("bias", bias, torch.bfloat16, (N,))
+    if residual is not None:
+        _vector("residual", residual, dt, (M, N))
+    out = _output("out", out, (M, N), dt, a)
+    with _one_device(a, b, bias, residual, out):
+        rc = lib().gemm_bf16_epilogue(a.data_ptr(), b.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(),
+                                      int(dt == torch.bfloat16), ACTIVATIONS[activation], M, N, K,
+                                      _stream_handle(stream, a))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return out
