@@ -467,8 +467,18 @@ ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_
  *             the sequence's positions, gives NaN in that sequence's O and LSE
  *   O         device, [B, Hq, D]: fp32, or bf16 if o_bf16 != 0      written
  *   LSE       device, fp32 [B, Hq]                                  written
- *   Hq % Hkv == 0; scale >= 0, finite; O and LSE 16-byte aligned and apart
- *   from each other and from every input (TA_ERR_ALIASING)
+ *   Hq % Hkv == 0, Hq <= 65536, B * Hq < 2^24 (else TA_ERR_INVALID_SHAPE);
+ *   scale >= 0, finite; O and LSE 16-byte aligned and apart from each other and
+ *   from every input (TA_ERR_ALIASING)
+ *   num_parts 0..4096 (else TA_ERR_INVALID_SHAPE): the cached positions of the
+ *             whole batch, whatever its lengths, are divided evenly over this
+ *             many workgroups, and a second kernel joins the results of the heads
+ *             that the division cuts, in order, through `workspace` (device,
+ *             16-byte aligned, at least attn_paged_workspace_bytes(...) bytes,
+ *             owned by the caller, its contents on entry of no account, no
+ *             overlap with any other argument; TA_ERR_WORKSPACE if NULL or
+ *             smaller).  0: one workgroup per sequence and key/value head (and
+ *             32 query heads of it), no workspace
  *
  * Entries of page_table past a sequence's last page, and what the caches hold
  * past its last position, are never used.  Scores and sums are fp32; the softmax
@@ -480,7 +490,15 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
                             const float *v_scale, const int *page_table, const int *seq_lens,
                             void *O, int o_bf16, float *LSE, int B, int Hq, int Hkv, int D,
                             int num_pages, int page_size, int max_pages, float scale,
+                            int num_parts, void *workspace, size_t workspace_bytes,
                             void *stream);
+
+/* Workspace bytes attn_decode_paged needs for num_parts (0 for none).  No HIP call. */
+ta_status attn_paged_workspace_bytes(int Hq, int Hkv, int D, int num_parts, size_t *bytes);
+
+/* A part count for attn_decode_paged, from the table's capacity.  No HIP call. */
+ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages,
+                          int *num_parts);
 
 /* Activations of gemm_bf16_epilogue */
 typedef enum {

@@ -5,10 +5,15 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "paged_plan.h"
 #include "tileattn.h"
 
 namespace {
 
+using namespace tileattn_detail;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -90,70 +95,555 @@ struct PagedArgs {
     const float *ks, *vs;
     const int *table, *lens;
     void *O;
-    float *LSE;
+    float *LSE, *W;
+    int o_bf16;
     int B, Hq, Hkv, num_pages, page_shift, max_pages;
-    float scale;
+    int group, rows, blocks;   // Hq / Hkv; of them per workgroup; row blocks of a group
+    int parts;                 // 0: a workgroup per (sequence, K/V head, row block)
+    float c;                   // scale * log2(e)
 };
 
-template <int D, bool E4M3>
-__device__ __forceinline__ float cache_at(const void *c, size_t row, int d)
+constexpr int NW = PAGED_NW;
+constexpr float LN2 = 0.69314718055994530942f;
+constexpr float RESCALE_SLACK = 8.f;
+
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
 {
-    if (E4M3)
-        return __builtin_amdgcn_cvt_f32_fp8(((const uint8_t *)c)[row * D + d], 0);
-    return __uint_as_float((uint32_t)((const uint16_t *)c)[row * D + d] << 16);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// One wave per query row: the lanes share a key's dims, one key after the other.
-template <int D, bool E4M3, bool OBF16>
-__global__ __launch_bounds__(64) void attn_paged_kernel(PagedArgs a)
+// x over the four lanes l, l ^ 16, l ^ 32, l ^ 48 that hold one row
+__device__ __forceinline__ float max_row(float x)
 {
-    constexpr int PL = D / 64;
-    const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / (a.Hq / a.Hkv);
-    const int lane = threadIdx.x;
-    const int len = a.lens[b];
-    const float ks = (a.ks ? a.ks[h] : 1.f) * a.scale, vs = a.vs ? a.vs[h] : 1.f;
-    float q[PL], acc[PL], m = -INFINITY, l = 0.f;
+    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float sum_row(float x)
+{
+    u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// two e4m3 numbers (bytes 0, 1, or 2, 3 with HI) as bf16, exactly
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3_bf16(uint32_t w)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HI));
+}
+
+// the high halves of (lo, hi) as a pair, and the low ones
+__device__ __forceinline__ uint32_t high16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302); }
+__device__ __forceinline__ uint32_t low16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100); }
+
+// The batch's tiles, and the sequence that tile t (of all) lies in: every wave
+// finds both by itself from the lengths.  HR: K/V heads times row blocks.
+struct Place {
+    uint32_t b, first;   // the sequence, and its first tile
+};
+
+__device__ __forceinline__ uint32_t all_tiles(const PagedArgs &a, uint32_t HR, int cap, int tile, int lane)
+{
+    uint32_t n = 0;
+    for (int i = lane; i < a.B; i += 64)
+        n += paged_tiles(a.lens[i], cap, tile);
 #pragma unroll
-    for (int i = 0; i < PL; ++i) {
-        q[i] = __uint_as_float((uint32_t)a.Q[b * a.q_stride + (size_t)hq * D + lane * PL + i] << 16);
-        acc[i] = 0.f;
-    }
-    bool bad = len < 0 || len > (int64_t)a.max_pages << a.page_shift;
-    for (int t = 0; !bad && t < len; ++t) {
-        const int page = a.table[(size_t)b * a.max_pages + (t >> a.page_shift)];
-        if (page < 0 || page >= a.num_pages) {
-            bad = true;
-            break;
+    for (int o = 32; o; o >>= 1)
+        n += __shfl_xor(n, o);
+    return __builtin_amdgcn_readfirstlane(n) * HR;
+}
+
+__device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int cap, int tile, int lane, uint32_t t)
+{
+    uint32_t base = 0;
+    for (int i0 = 0; i0 < a.B; i0 += 64) {
+        const uint32_t n = i0 + lane < a.B ? paged_tiles(a.lens[i0 + lane], cap, tile) : 0;
+        uint32_t s = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t u = __shfl_up(s, o);
+            s += lane >= o ? u : 0;
         }
-        const size_t row = (((size_t)page * a.Hkv + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1));
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < PL; ++i)
-            s += q[i] * cache_at<D, E4M3>(a.K, row, lane * PL + i);
-#pragma unroll
-        for (int o = 32; o; o >>= 1)
-            s += __shfl_xor(s, o);
-        s *= ks;
-        const float mn = fmaxf(m, s);
-        const float al = m == mn ? 1.f : __expf(m - mn), p = s == mn ? 1.f : __expf(s - mn);
-        m = mn;
-        l = l * al + p;
-#pragma unroll
-        for (int i = 0; i < PL; ++i)
-            acc[i] = acc[i] * al + p * cache_at<D, E4M3>(a.V, row, lane * PL + i);
+        const uint64_t after = __builtin_amdgcn_ballot_w64(base + s * HR > t);   // sequences that end past t
+        if (after) {
+            const int l = __builtin_ctzll(after);
+            const uint32_t end = __builtin_amdgcn_readlane(s, l), own = __builtin_amdgcn_readlane(n, l);
+            return {(uint32_t)(i0 + l), base + (end - own) * HR};
+        }
+        base += __builtin_amdgcn_readlane(s, 63) * HR;
     }
-    const size_t r = (size_t)b * a.Hq + hq;
-    const float inv = bad ? NAN : len == 0 ? 0.f : vs / l;
-#pragma unroll
-    for (int i = 0; i < PL; ++i) {
-        const float o = acc[i] * inv;
-        if (OBF16)
-            ((uint16_t *)a.O)[r * D + lane * PL + i] = (uint16_t)pack_bf16(o, 0.f);
-        else
-            ((float *)a.O)[r * D + lane * PL + i] = o;
+    return {0, 0};   // (t is one of the tiles)
+}
+
+// Attention of one new token per sequence.  HBM bounds it: every key and value is
+// read once and feeds the few query heads of its group, the columns of
+// v_mfma_f32_16x16x32_bf16: S^T = K Q^T, O^T += V^T P^T.
+//
+//  * K and V go from memory to the registers they are used in, nothing through
+//    LDS: a lane's 16 bytes of a K row are its operand of the scores as they are
+//    (8 dims of one key).  Of V a lane loads the same 8 dims of eight keys, the
+//    keys whose weights the scores left in it, and transposes the 8 x 8 block
+//    with byte permutes: operand j of O^T is then dims 8 c16 + j of all lanes.
+//  * A wave takes KS keys a step, on its own, with its own running maximum and
+//    sums; the next K is loaded under the softmax and the product with V, the
+//    next V under the scores.  The NW waves of a workgroup meet in LDS at the end
+//    of a head's keys.
+//  * The positions of the whole batch, head by head, are one list of tiles of NW
+//    steps; each workgroup takes an even share of it (parts), so a batch of mixed
+//    lengths occupies the GPU as one of equal ones does, without the host knowing
+//    the lengths.  Heads that a share's ends cut leave partial results for
+//    attn_paged_merge_kernel.
+//  * A 16-key block lies in one page (page_size >= 16), so pages are looked up in
+//    scalar registers, a step ahead.
+template <int D, bool E4M3, int RT>
+__global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
+{
+    constexpr int KS = paged_step(D, E4M3);      // keys per wave and step
+    constexpr int KB = KS / 16;                  // blocks of 16 keys
+    constexpr int TILE = KS * NW;
+    constexpr int KK = D / 32;                   // k-steps of the scores
+    constexpr int ROW = D * (E4M3 ? 1 : 2);      // bytes of a key
+    constexpr int KL = ROW / 64;                 // 16-byte loads per lane and key block
+    constexpr int DJ = D / 16;                   // dims of a value per lane
+    constexpr int VW = DJ * (E4M3 ? 1 : 2) / 4;  // dwords of them
+    __shared__ __attribute__((aligned(16))) float po[NW][16 * RT][D];
+    __shared__ float ml[NW][2][16 * RT];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const int cap = a.max_pages << a.page_shift;
+    const uint32_t HR = a.Hkv * a.blocks;
+
+    // the tiles of this workgroup: from tile t of head `hr` (K/V head and row
+    // block) of sequence b, `left` of them
+    uint32_t b, hr, t, left;
+    if (a.parts) {
+        const uint32_t n = all_tiles(a, HR, cap, TILE, lane), used = paged_parts_used(n, a.parts);
+        if (blockIdx.x >= used)
+            return;
+        const uint32_t begin = paged_part_begin(n, used, blockIdx.x);
+        left = paged_part_begin(n, used, blockIdx.x + 1) - begin;
+        const Place at = place_of(a, HR, cap, TILE, lane, begin);
+        const uint32_t per = paged_tiles(a.lens[at.b], cap, TILE);
+        b = at.b;
+        hr = (begin - at.first) / per;
+        t = (begin - at.first) % per;
+    } else {
+        b = blockIdx.x / HR;
+        hr = blockIdx.x % HR;
+        t = 0;
+        left = ~0u;
     }
-    if (lane == 0)
-        a.LSE[r] = bad ? NAN : len == 0 ? -INFINITY : m + logf(l);
+
+    for (;;) {
+        const int len = __builtin_amdgcn_readfirstlane(a.lens[b]);
+        const bool bad_len = len < 0 || len > cap;
+        const uint32_t per = paged_tiles(len, cap, TILE);
+        const uint32_t take = min(left, per - t);
+        const int h = hr / a.blocks, r0 = (hr % a.blocks) * a.rows;
+        const int rows = min(a.rows, a.group - r0);      // query rows of this block
+        const size_t row0 = (size_t)b * a.Hq + (size_t)h * a.group + r0;
+        const int k_lo = t * TILE, k_hi = bad_len ? 0 : min(len, (int)((t + take) * TILE));
+        const int first = k_lo + wave * KS;
+        const int steps = first < k_hi ? (k_hi - first + TILE - 1) / TILE : 0;
+        const int *const table = a.table + (size_t)b * a.max_pages;
+
+        // Q as the B operand: row c16, the dims of the lane's K loads (rows past
+        // the last read the last; they are never stored)
+        bf16x8 q[RT][KK];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const uint16_t *qp = a.Q + b * a.q_stride + (size_t)(h * a.group + r0 + min(16 * i + c16, rows - 1)) * D;
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk)
+                q[i][kk] = __builtin_bit_cast(
+                    bf16x8, *(const u32x4 *)(qp + (E4M3 ? 64 * (kk >> 1) + 16 * g + 8 * (kk & 1) : 32 * kk + 8 * g)));
+        }
+        const float c = a.c * (a.ks ? a.ks[h] : 1.f);
+
+        f32x4 acc[RT][DJ];
+        float m_run[RT], l_run[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            m_run[i] = -INFINITY;
+            l_run[i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < DJ; ++j)
+                acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // the rows of this head in a step's blocks: from the page's first row,
+        // bytes from the cache's start; a block past the last key is the last one
+        const int last_block = (k_hi - 1) >> 4;
+        auto lookup = [&](int s, int (&page)[KB]) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const int blk = min(((first + s * TILE) >> 4) + kb, last_block);
+                page[kb] = paged_checked(table[blk >> (a.page_shift - 4)], a.num_pages);
+            }
+        };
+        auto block_at = [&](int s, int kb, int page) {
+            const int blk = min(((first + s * TILE) >> 4) + kb, last_block);
+            const int in = (blk << 4) & ((1 << a.page_shift) - 1);
+            return (((size_t)max(page, 0) * a.Hkv + h) << a.page_shift) * ROW + (size_t)in * ROW;
+        };
+        u32x4 kr[KB][KL];
+        uint32_t vr[KB][4][VW];
+        auto load_k = [&](int s, const int (&page)[KB]) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const unsigned char *p = (const unsigned char *)a.K + block_at(s, kb, page[kb]);
+#pragma unroll
+                for (int i = 0; i < KL; ++i)
+                    kr[kb][i] = *(const u32x4 *)(p + (uint32_t)(c16 * ROW + 64 * i + 16 * g));
+            }
+        };
+        auto load_v = [&](int s, const int (&page)[KB]) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) {
+                const unsigned char *p = (const unsigned char *)a.V + block_at(s, kb, page[kb]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const unsigned char *e = p + (uint32_t)((4 * g + i) * ROW + c16 * (4 * VW));
+                    if constexpr (VW == 4) {
+                        const u32x4 x = *(const u32x4 *)e;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w)
+                            vr[kb][i][w] = x[w];
+                    } else if constexpr (VW == 2) {
+                        const u32x2 x = *(const u32x2 *)e;
+                        vr[kb][i][0] = x[0];
+                        vr[kb][i][1] = x[1];
+                    } else {
+                        vr[kb][i][0] = *(const uint32_t *)e;
+                    }
+                }
+            }
+        };
+
+        int page[KB], next[KB];
+        if (steps > 0) {
+            lookup(0, page);
+            load_k(0, page);
+            load_v(0, page);
+            if (steps > 1)
+                lookup(1, next);
+        }
+        for (int s = 0; s < steps; ++s) {
+            const int key0 = first + s * TILE;
+            const bool tail = key0 + KS > k_hi;      // uniform
+            // scores: lane holds keys 16 kb + 4 g + r of row c16
+            f32x4 sc[RT][KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    sc[i][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int kk = 0; kk < KK; ++kk) {
+                        bf16x8 k;
+                        if constexpr (E4M3) {
+                            const uint32_t w0 = kr[kb][kk >> 1][2 * (kk & 1)], w1 = kr[kb][kk >> 1][2 * (kk & 1) + 1];
+                            k = __builtin_bit_cast(bf16x8, u32x4{e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
+                                                                 e4m3_bf16<false>(w1), e4m3_bf16<true>(w1)});
+                        } else {
+                            k = __builtin_bit_cast(bf16x8, kr[kb][kk]);
+                        }
+                        sc[i][kb] = mfma(k, q[i][kk], sc[i][kb]);
+                    }
+                }
+            bool bad[KB];
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                bad[kb] = page[kb] < 0;
+            if (s + 1 < steps)
+                load_k(s + 1, next);
+            // a page outside the pool makes its keys' scores NaN, and so the row
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                if (bad[kb])
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+                        sc[i][kb] = f32x4{NAN, NAN, NAN, NAN};
+
+            // V as the A operand of O^T: k-slot of lane group g <-> keys 32 kp + 4 g
+            // + (0..3) and 32 kp + 16 + 4 g + (0..3), as the scores left the weights
+            if (tail) {   // what lies behind the last key may be anything
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int w = 0; w < VW; ++w)
+                            vr[kb][i][w] = key0 + 16 * kb + 4 * g + i < k_hi ? vr[kb][i][w] : 0u;
+            }
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if (tail)
+                            sc[i][kb][r] = key0 + 16 * kb + 4 * g + r < k_hi ? sc[i][kb][r] : -INFINITY;
+                        mx = fmaxf(mx, sc[i][kb][r]);
+                    }
+                mx = max_row(mx);
+                const float m_step = mx == -INFINITY ? -INFINITY : mx * c;
+                if (__builtin_amdgcn_ballot_w64(m_step > m_run[i] + RESCALE_SLACK)) {
+                    const float m_new = fmaxf(m_run[i], m_step);
+                    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[i] - m_new);
+                    m_run[i] = m_new;
+                    l_run[i] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < DJ; ++j)
+                        acc[i][j] *= alpha;
+                }
+                const float m_use = m_run[i] == -INFINITY ? 0.f : m_run[i];
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][kb][r], c, -m_use));
+                        if (tail)   // (scale 0 makes a masked score NaN, not -inf)
+                            p = key0 + 16 * kb + 4 * g + r < k_hi ? p : 0.f;
+                        sc[i][kb][r] = p;
+                        l_run[i] += p;
+                    }
+            }
+#pragma unroll
+            for (int kp = 0; kp < KB / 2; ++kp) {
+                // The weights as bf16 numbers that add up to 16 of their 24 bits, or
+                // all of them: what is cut off here would be the largest error of O,
+                // and the matrix cores have the time
+                bf16x8 p[RT][3];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        w[r] = __float_as_uint(sc[i][2 * kp + (r >> 2)][r & 3]);
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) {
+                        p[i][n] = __builtin_bit_cast(bf16x8, u32x4{high16(w[0], w[1]), high16(w[2], w[3]),
+                                                                   high16(w[4], w[5]), high16(w[6], w[7])});
+#pragma unroll
+                        for (int r = 0; r < 8; ++r)
+                            w[r] = __float_as_uint(__uint_as_float(w[r]) - __uint_as_float(w[r] & 0xFFFF0000u));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < DJ; j += 2) {
+                    uint32_t x0[4], x1[4];   // dims j and j + 1, keys in pairs
+#pragma unroll
+                    for (int pr = 0; pr < 4; ++pr) {
+                        const auto &e = vr[2 * kp + (pr >> 1)][2 * (pr & 1)], &o = vr[2 * kp + (pr >> 1)][2 * (pr & 1) + 1];
+                        if constexpr (E4M3) {
+                            // bytes j, j + 1 of both keys, paired by dim, then as bf16
+                            const uint32_t w = __builtin_amdgcn_perm(o[j >> 2], e[j >> 2], j & 2 ? 0x07030602 : 0x05010400);
+                            x0[pr] = e4m3_bf16<false>(w);
+                            x1[pr] = e4m3_bf16<true>(w);
+                        } else {
+                            x0[pr] = low16(e[j >> 1], o[j >> 1]);
+                            x1[pr] = high16(e[j >> 1], o[j >> 1]);
+                        }
+                    }
+                    const bf16x8 v0 = __builtin_bit_cast(bf16x8, u32x4{x0[0], x0[1], x0[2], x0[3]});
+                    const bf16x8 v1 = __builtin_bit_cast(bf16x8, u32x4{x1[0], x1[1], x1[2], x1[3]});
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            acc[i][j] = mfma(v0, p[i][n], acc[i][j]);
+                            acc[i][j + 1] = mfma(v1, p[i][n], acc[i][j + 1]);
+                        }
+                        if (!a.o_bf16) {
+                            acc[i][j] = mfma(v0, p[i][2], acc[i][j]);
+                            acc[i][j + 1] = mfma(v1, p[i][2], acc[i][j + 1]);
+                        }
+                    }
+                }
+            }
+            if (s + 1 < steps) {
+                load_v(s + 1, next);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+                    page[kb] = next[kb];
+                if (s + 2 < steps)
+                    lookup(s + 2, next);
+            }
+        }
+
+        // The waves' sums meet in LDS, in wave order.  Lane: row c16, dims
+        // DJ (4 g + r) + j; 16-byte chunk ch of row x at ch ^ x.
+        __syncthreads();   // (the head before this one has been read)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const float l = sum_row(l_run[i]);
+            const int x = 16 * i + c16;
+            if (x < rows) {
+                if (g == 0) {
+                    ml[wave][0][x] = m_run[i];
+                    ml[wave][1][x] = l;
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int j = 0; j < DJ; j += 4)
+                        *(f32x4 *)&po[wave][x][4 * (((DJ * (4 * g + r) + j) / 4) ^ c16)] =
+                            f32x4{acc[i][j][r], acc[i][j + 1][r], acc[i][j + 2][r], acc[i][j + 3][r]};
+            }
+        }
+        __syncthreads();
+        const bool begins = t == 0, ends = t + take == per;
+        float *const rec = begins && ends ? nullptr : a.W + (2 * (size_t)blockIdx.x + begins) * paged_record(a.rows, D);
+        const float vs = a.vs ? a.vs[h] : 1.f;
+        for (int e = tid; e < rows * (D / 4); e += 64 * NW) {
+            const int x = e / (D / 4), ch = e % (D / 4);
+            float m = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                m = fmaxf(m, ml[w][0][x]);
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float mw = ml[w][0][x];
+                const float f = mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m);
+                l += f * ml[w][1][x];
+                o += f * *(const f32x4 *)&po[w][x][4 * (ch ^ (x & 15))];
+            }
+            if (rec) {
+                *(f32x4 *)(rec + (size_t)x * D + 4 * ch) = o;
+                if (ch == 0) {
+                    rec[((size_t)(a.rows + 3) & ~3) * D + x] = m;
+                    rec[((size_t)(a.rows + 3) & ~3) * (D + 1) + x] = l;
+                }
+            } else {
+                o *= bad_len ? NAN : l == 0.f ? 0.f : vs / l;
+                const size_t at = (row0 + x) * D + 4 * ch;
+                if (a.o_bf16)
+                    *(u32x2 *)((uint16_t *)a.O + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+                else
+                    *(f32x4 *)((float *)a.O + at) = o;
+                if (ch == 0)
+                    a.LSE[row0 + x] = bad_len ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+            }
+        }
+
+        left -= take;
+        if (!a.parts || left == 0)
+            return;
+        t = 0;
+        if (++hr == HR) {
+            hr = 0;
+            ++b;
+        }
+    }
+}
+
+// Joins the partial results of the heads that were cut: a workgroup per
+// (sequence, K/V head, row block), its threads in groups that take every
+// n-th record, then in LDS.
+constexpr int MERGE_T = 512;
+template <int D>
+__global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, int tile)
+{
+    __shared__ __attribute__((aligned(16))) float so[MERGE_T][4];
+    __shared__ float sm[MERGE_T], sl[MERGE_T];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int cap = a.max_pages << a.page_shift;
+    const uint32_t HR = a.Hkv * a.blocks, b = blockIdx.x / HR, hr = blockIdx.x % HR;
+    uint32_t n = 0, before = 0;   // tiles of the batch, and of the sequences before b
+    for (int i = lane; i < a.B; i += 64) {
+        const uint32_t x = paged_tiles(a.lens[i], cap, tile);
+        n += x;
+        before += (uint32_t)i < b ? x : 0;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        n += __shfl_xor(n, o);
+        before += __shfl_xor(before, o);
+    }
+    n = __builtin_amdgcn_readfirstlane(n) * HR;
+    const uint32_t per = paged_tiles(a.lens[b], cap, tile);
+    const uint32_t t0 = __builtin_amdgcn_readfirstlane(before) * HR + hr * per;
+    const uint32_t used = paged_parts_used(n, a.parts);
+    const uint32_t p0 = paged_part_of(n, used, t0), p1 = paged_part_of(n, used, t0 + per - 1);
+    if (p0 == p1)
+        return;   // a head that one workgroup took whole
+    const int h = hr / a.blocks, r0 = (hr % a.blocks) * a.rows;
+    const int rows = min(a.rows, a.group - r0);
+    const size_t row0 = (size_t)b * a.Hq + (size_t)h * a.group + r0;
+    const size_t pad = (size_t)(a.rows + 3) & ~3, rec = paged_record(a.rows, D);
+    const float vs = a.vs ? a.vs[h] : 1.f;
+
+    const int items = rows * (D / 4);            // 16-byte chunks of the head's rows
+    // threads per group of records: a power of two of them work on one chunk
+    int per_item = 1;
+    while (per_item < 16 && items * per_item * 2 <= MERGE_T)
+        per_item *= 2;
+    const int width = MERGE_T / per_item;        // chunks at a time
+    const int k = tid / width;
+    for (int e0 = 0; e0 < items; e0 += width) {
+        const int e = e0 + tid % width;
+        const int x = min(e, items - 1) / (D / 4), ch = min(e, items - 1) % (D / 4);
+        float m = -INFINITY, l = 0.f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        constexpr int U = 4;                     // records in flight
+        for (uint32_t p = p0 + k; p <= p1; p += U * per_item) {
+            float mp[U], lp[U];
+            f32x4 op[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t pu = min(p + u * per_item, p1);
+                const float *r = a.W + (2 * (size_t)pu + (pu == p0)) * rec;
+                op[u] = *(const f32x4 *)(r + (size_t)x * D + 4 * ch);
+                mp[u] = r[pad * D + x];
+                lp[u] = r[pad * (D + 1) + x];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (p + u * per_item > p1)
+                    break;
+                const float mn = fmaxf(m, mp[u]);
+                const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                const float f1 = mp[u] == mn ? 1.f : __builtin_amdgcn_exp2f(mp[u] - mn);
+                m = mn;
+                l = l * f0 + lp[u] * f1;
+                o = o * f0 + op[u] * f1;
+            }
+        }
+        __syncthreads();
+        *(f32x4 *)so[tid] = o;
+        sm[tid] = m;
+        sl[tid] = l;
+        __syncthreads();
+        if (k == 0 && e < items) {
+            for (int i = 1; i < per_item; ++i) {
+                const int s = tid + i * width;
+                const float mn = fmaxf(m, sm[s]);
+                const float f0 = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+                const float f1 = sm[s] == mn ? 1.f : __builtin_amdgcn_exp2f(sm[s] - mn);
+                m = mn;
+                l = l * f0 + sl[s] * f1;
+                o = o * f0 + *(const f32x4 *)so[s] * f1;
+            }
+            o *= l == 0.f ? 0.f : vs / l;
+            const size_t at = (row0 + x) * D + 4 * ch;
+            if (a.o_bf16)
+                *(u32x2 *)((uint16_t *)a.O + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
+            else
+                *(f32x4 *)((float *)a.O + at) = o;
+            if (ch == 0)
+                a.LSE[row0 + x] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+        }
+    }
 }
 
 bool misaligned(const void *p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
@@ -190,6 +680,16 @@ size_t cache_bytes(int Hkv, int D, int num_pages, int page_size, int cache_e4m3)
 {
     const unsigned __int128 n = (unsigned __int128)num_pages * Hkv * page_size * D * (cache_e4m3 ? 1 : 2);
     return n > (1ull << 62) ? (size_t)1 << 62 : (size_t)n;
+}
+
+bool heads_ok(int B, int Hq, int Hkv)
+{
+    return B >= 1 && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 && Hq <= 1 << 16 && (int64_t)B * Hq < 1ll << 24;
+}
+
+size_t workspace_need(int group, int D, int num_parts)
+{
+    return (size_t)num_parts * 2 * paged_record(paged_block_rows(group), D) * 4;
 }
 
 }  // namespace
@@ -240,7 +740,7 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
                             const float *v_scale, const int *page_table, const int *seq_lens,
                             void *O, int o_bf16, float *LSE, int B, int Hq, int Hkv, int D,
                             int num_pages, int page_size, int max_pages, float scale,
-                            void *stream)
+                            int num_parts, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!Q || !K_cache || !V_cache || !page_table || !seq_lens || !O || !LSE)
         return TA_ERR_NULL_POINTER;
@@ -248,8 +748,12 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
     if (rc != TA_OK)
         return rc;
     const int64_t row = (int64_t)Hq * D;
-    if (Hq < 1 || Hq % Hkv || q_stride < row || q_stride % 8 || q_stride > 1ll << 30 || Hq > 1 << 16 ||
-        (int64_t)B * Hq >= 1ll << 24)
+    if (!heads_ok(B, Hq, Hkv) || q_stride < row || q_stride % 8 || q_stride > 1ll << 30 || num_parts < 0 ||
+        num_parts > PAGED_MAX_PARTS)
+        return TA_ERR_INVALID_SHAPE;
+    const int group = Hq / Hkv, blocks = paged_row_blocks(group);
+    const int tile = paged_step(D, cache_e4m3) * PAGED_NW;
+    if (((int64_t)max_pages * page_size / tile + 1) * B * Hkv * blocks >= 1ll << 31)   // tiles in 32 bits
         return TA_ERR_INVALID_SHAPE;
     if (misaligned(Q) || misaligned(K_cache) || misaligned(V_cache) || misaligned(O) || misaligned(LSE) ||
         misaligned(page_table, 4) || misaligned(seq_lens, 4) || misaligned(k_scale, 4) || misaligned(v_scale, 4))
@@ -257,7 +761,9 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
     if (!(scale >= 0.f) || !(scale <= 3.402823466e+38f))
         return TA_ERR_INVALID_SCALE;
     const size_t cb = cache_bytes(Hkv, D, num_pages, page_size, cache_e4m3);
+    const size_t need = workspace_need(group, D, num_parts);
     const Span o = {O, (size_t)B * row * (o_bf16 ? 2 : 4)}, l = {LSE, (size_t)B * Hq * 4};
+    const Span w = {need ? workspace : nullptr, need};
     const Span in[] = {{Q, (size_t)((B - 1) * q_stride + row) * 2}, {K_cache, cb}, {V_cache, cb},
                        {page_table, (size_t)B * max_pages * 4}, {seq_lens, (size_t)B * 4},
                        {k_scale, (size_t)Hkv * 4}, {v_scale, (size_t)Hkv * 4}};
@@ -266,17 +772,60 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
     for (const Span &s : in)
         if (overlaps(o, s) || overlaps(l, s))
             return TA_ERR_ALIASING;
+    if (need) {
+        if (!workspace || workspace_bytes < need)
+            return TA_ERR_WORKSPACE;
+        if (misaligned(workspace))
+            return TA_ERR_MISALIGNED;
+        if (overlaps(w, o) || overlaps(w, l))
+            return TA_ERR_ALIASING;
+        for (const Span &s : in)
+            if (overlaps(w, s))
+                return TA_ERR_ALIASING;
+    }
     const PagedArgs a = {(const uint16_t *)Q, q_stride, K_cache, V_cache, k_scale, v_scale, page_table, seq_lens, O,
-                         LSE, B, Hq, Hkv, num_pages, __builtin_ctz(page_size), max_pages, scale};
-    const dim3 grid((unsigned)(B * Hq)), block(64);
+                         LSE, (float *)workspace, o_bf16 != 0, B, Hq, Hkv, num_pages, __builtin_ctz(page_size),
+                         max_pages, group, paged_block_rows(group), blocks, num_parts, scale * 1.44269504088896340736f};
+    const dim3 grid((unsigned)(num_parts ? num_parts : B * Hkv * blocks)), block(64 * NW);
     hipStream_t s = (hipStream_t)stream;
+    const bool two = a.rows > 16;
     const auto kernel =
-        D == 64 ? (cache_e4m3 ? (o_bf16 ? attn_paged_kernel<64, true, true> : attn_paged_kernel<64, true, false>)
-                              : (o_bf16 ? attn_paged_kernel<64, false, true> : attn_paged_kernel<64, false, false>))
-                : (cache_e4m3 ? (o_bf16 ? attn_paged_kernel<128, true, true> : attn_paged_kernel<128, true, false>)
-                              : (o_bf16 ? attn_paged_kernel<128, false, true> : attn_paged_kernel<128, false, false>));
+        D == 64 ? (cache_e4m3 ? (two ? attn_paged_kernel<64, true, 2> : attn_paged_kernel<64, true, 1>)
+                              : (two ? attn_paged_kernel<64, false, 2> : attn_paged_kernel<64, false, 1>))
+                : (cache_e4m3 ? (two ? attn_paged_kernel<128, true, 2> : attn_paged_kernel<128, true, 1>)
+                              : (two ? attn_paged_kernel<128, false, 2> : attn_paged_kernel<128, false, 1>));
     hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
-    return hipGetLastError() == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && num_parts) {
+        const auto merge = D == 64 ? attn_paged_merge_kernel<64> : attn_paged_merge_kernel<128>;
+        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks)), dim3(MERGE_T), 0, s, a, tile);
+        e = hipGetLastError();
+    }
+    return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+}
+
+ta_status attn_paged_workspace_bytes(int Hq, int Hkv, int D, int num_parts, size_t *bytes)
+{
+    if (!bytes)
+        return TA_ERR_NULL_POINTER;
+    if (!heads_ok(1, Hq, Hkv) || D < 1 || num_parts < 0 || num_parts > PAGED_MAX_PARTS)
+        return TA_ERR_INVALID_SHAPE;
+    if (D != 64 && D != 128)
+        return TA_ERR_UNSUPPORTED;
+    *bytes = workspace_need(Hq / Hkv, D, num_parts);
+    return TA_OK;
+}
+
+ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages, int *num_parts)
+{
+    if (!num_parts)
+        return TA_ERR_NULL_POINTER;
+    if (!heads_ok(B, Hq, Hkv) || D < 1 || page_size < 1 || max_pages < 1)
+        return TA_ERR_INVALID_SHAPE;
+    if (D != 64 && D != 128)
+        return TA_ERR_UNSUPPORTED;
+    *num_parts = (int64_t)max_pages * page_size <= 512 ? 0 : 512;
+    return TA_OK;
 }
 
 }  // extern "C"

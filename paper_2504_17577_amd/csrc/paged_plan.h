@@ -1,0 +1,63 @@
+// Integer logic of the paged cache's kernels: where a position lies, and how the
+// cached positions of a batch are divided over workgroups.  No HIP: the kernels
+// and host code (its tests too) share it.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define PAGED_FN __host__ __device__ inline
+#else
+#define PAGED_FN inline
+#endif
+
+namespace tileattn_detail {
+
+constexpr int PAGED_NW = 4;            // waves of an attention workgroup
+constexpr int PAGED_MAX_PARTS = 4096;
+constexpr int PAGED_MAX_ROWS = 32;     // query heads of a group that one workgroup takes
+
+// keys of a wave's step: 16 KB of K and V in flight per wave, 8 KB for 64 dims of 8 bits
+PAGED_FN constexpr int paged_step(int D, bool e4m3) { return D == 128 && !e4m3 ? 32 : 64; }
+
+// Tiles of one sequence, counted as at least one (a sequence of no positions, or
+// of a length outside 0..cap, has results to be written too).
+PAGED_FN uint32_t paged_tiles(int len, int cap, int tile)
+{
+    return len <= 0 || len > cap ? 1u : (uint32_t)(len - 1) / (uint32_t)tile + 1u;
+}
+
+// n tiles in `parts` parts, as even as they go: the first n % parts get one more
+PAGED_FN uint32_t paged_part_begin(uint32_t n, uint32_t parts, uint32_t p)
+{
+    const uint32_t r = n % parts;
+    return n / parts * p + (p < r ? p : r);
+}
+
+PAGED_FN uint32_t paged_part_of(uint32_t n, uint32_t parts, uint32_t t)
+{
+    const uint32_t q = n / parts, r = n % parts, big = r * (q + 1);
+    return t < big ? t / (q + 1) : r + (t - big) / q;
+}
+
+// The parts that n tiles are cut into where `parts` workgroups run
+PAGED_FN uint32_t paged_parts_used(uint32_t n, uint32_t parts) { return n < parts ? n : parts; }
+
+// A page index of the table, or -1 for one outside the pool
+PAGED_FN int paged_checked(int page, int num_pages) { return page >= 0 && page < num_pages ? page : -1; }
+
+// Row blocks of a group of `group` query heads, and the heads in each
+PAGED_FN int paged_row_blocks(int group) { return (group + PAGED_MAX_ROWS - 1) / PAGED_MAX_ROWS; }
+PAGED_FN int paged_block_rows(int group)
+{
+    const int rb = paged_row_blocks(group);
+    return (group + rb - 1) / rb;
+}
+
+// Partial results: part p has two records, 2 p for what it does of a head that an
+// earlier part began and 2 p + 1 for one that it begins and a later part goes on
+// with.  A record is [rows][D] sums, [rows] maxima and [rows] weights in fp32,
+// rows rounded up to four (16-byte records).
+PAGED_FN uint64_t paged_record(int rows, int D) { return (uint64_t)((rows + 3) & ~3) * (uint64_t)(D + 2); }
+
+}  // namespace tileattn_detail

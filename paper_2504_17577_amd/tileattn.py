@@ -107,7 +107,12 @@ def lib():
     L.kv_cache_append.restype = i
     L.kv_cache_append.argtypes = [p, p, ctypes.c_int64, ctypes.c_int64, p, p, p, p, i, p, p, p] + [i] * 7 + [p]
     L.attn_decode_paged.restype = i
-    L.attn_decode_paged.argtypes = [p, ctypes.c_int64, p, p, i, p, p, p, p, p, i, p] + [i] * 7 + [ctypes.c_float, p]
+    L.attn_decode_paged.argtypes = ([p, ctypes.c_int64, p, p, i, p, p, p, p, p, i, p] + [i] * 7
+                                    + [ctypes.c_float, i, p, ctypes.c_size_t, p])
+    L.attn_paged_workspace_bytes.restype = i
+    L.attn_paged_workspace_bytes.argtypes = [i] * 4 + [ctypes.POINTER(ctypes.c_size_t)]
+    L.attn_paged_plan.restype = i
+    L.attn_paged_plan.argtypes = [i] * 6 + [ctypes.POINTER(i)]
     L.gemm_bf16_epilogue.restype = i
     L.gemm_bf16_epilogue.argtypes = [p] * 5 + [i] * 5 + [p]
     L.ta_schedule.restype = i
@@ -776,14 +781,35 @@ def kv_cache_append(k, v, k_cache, v_cache, page_table, pos, seq=None, k_scale=N
     return k_cache, v_cache
 
 
+def attn_paged_workspace_bytes(Hq: int, Hkv: int, D: int, num_parts: int) -> int:
+    n = ctypes.c_size_t()
+    rc = lib().attn_paged_workspace_bytes(Hq, Hkv, D, num_parts, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
+def attn_paged_plan(B: int, Hq: int, Hkv: int, D: int, page_size: int, max_pages: int) -> int:
+    n = ctypes.c_int()
+    rc = lib().attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
 def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | None = None,
-                      k_scale=None, v_scale=None, out=None, lse=None, out_dtype=None, stream=None):
+                      k_scale=None, v_scale=None, num_parts: int | None = None, out=None, lse=None,
+                      workspace=None, out_dtype=None, stream=None):
     """O [B, Hq, D], LSE [B, Hq] (fp32) = attention of one new token per sequence,
     q [B, Hq, D] bf16 (a slice of a fused projection will do), over the first
     seq_lens[b] (int32 GPU tensor [B]) positions of its pages; caches, table and
     scales as kv_cache_append takes them.  ``scale`` defaults to 1/sqrt(D),
     ``out_dtype`` is torch.float32 (default) or torch.bfloat16.  A sequence of
-    length 0 gets O = 0 and LSE = -inf."""
+    length 0 gets O = 0 and LSE = -inf.  The batch's positions are divided over
+    ``num_parts`` workgroups (default attn_paged_plan); ``workspace``, a uint8 GPU
+    tensor of at least attn_paged_workspace_bytes(...) bytes, is allocated here if
+    needed and not given; it must stay alive until the launch has finished on
+    ``stream``."""
     o_dtype = torch.float32 if out_dtype is None else out_dtype
     if o_dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
@@ -798,12 +824,22 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
         scale = 1.0 / math.sqrt(D)
     out = _output("out", out, (B, Hq, D), o_dtype, q)
     lse = _output("lse", lse, (B, Hq), torch.float32, q)
-    with _one_device(q, k_cache, v_cache, page_table, seq_lens, k_scale, v_scale, out, lse):
+    if num_parts is None:
+        num_parts = attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages)
+    need = attn_paged_workspace_bytes(Hq, Hkv, D, num_parts)
+    if workspace is None and need:
+        workspace = _workspace(need, q, stream)
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda
+                                  or not workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous uint8 GPU tensor")
+    with _one_device(q, k_cache, v_cache, page_table, seq_lens, k_scale, v_scale, out, lse, workspace):
         rc = lib().attn_decode_paged(q.data_ptr(), q_stride, k_cache.data_ptr(), v_cache.data_ptr(),
                                      int(e4m3), _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(),
                                      seq_lens.data_ptr(), out.data_ptr(), int(o_dtype == torch.bfloat16),
                                      lse.data_ptr(), B, Hq, Hkv, D, num_pages, page_size, max_pages,
-                                     float(scale), _stream_handle(stream, q))
+                                     float(scale), num_parts, _ptr(workspace),
+                                     workspace.numel() if workspace is not None else 0,
+                                     _stream_handle(stream, q))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return out, lse

@@ -37,9 +37,10 @@ def test_append_refusals(change, status):
     assert rc == status, f"{change}: got {ta.STATUS.get(rc, rc)}, want {ta.STATUS[status]}"
 
 
-Q, LENS, O, LSE = (0x100000000 * i for i in range(11, 15))
+Q, LENS, O, LSE, WS = (0x100000000 * i for i in range(11, 16))
 ATTN = dict(Q=Q, q_stride=4096, KC=KC, VC=VC, e4m3=0, ks=None, vs=None, table=TAB, lens=LENS, O=O, o_bf16=0, LSE=LSE,
-            B=4, Hq=32, Hkv=8, D=128, num_pages=100, page=64, per=20, scale=0.1, stream=None)
+            B=4, Hq=32, Hkv=8, D=128, num_pages=100, page=64, per=20, scale=0.1, parts=64, ws=WS,
+            ws_bytes=1 << 20, stream=None)
 
 
 @no_gpu
@@ -50,11 +51,31 @@ ATTN = dict(Q=Q, q_stride=4096, KC=KC, VC=VC, e4m3=0, ks=None, vs=None, table=TA
     (dict(scale=-0.1), 5), (dict(scale=float("nan")), 5), (dict(scale=float("inf")), 5),
     (dict(O=Q + 4096), 6), (dict(O=KC), 6), (dict(LSE=VC + 64), 6), (dict(LSE=O + 16), 6), (dict(O=TAB - 16), 6),
     (dict(LSE=LENS - 16), 6), (dict(e4m3=1, ks=O), 6),
+    (dict(parts=-1), 2), (dict(parts=4097), 2), (dict(B=1 << 19, per=1 << 20), 2), (dict(Hq=1 << 17), 2),
+    (dict(ws=0), 8), (dict(ws_bytes=64 * 2 * 4 * 130 * 4 - 1), 8), (dict(ws=WS + 8), 4),
+    (dict(ws=KC + 4096), 6), (dict(ws=O), 6), (dict(ws=LSE - 4096), 6), (dict(ws=TAB), 6),
 ], ids=str)
 def test_attention_refusals(change, status):
     a = dict(ATTN, **change)
     rc = ta.lib().attn_decode_paged(*a.values())
     assert rc == status, f"{change}: got {ta.STATUS.get(rc, rc)}, want {ta.STATUS[status]}"
+
+
+def test_paged_workspace_and_plan():
+    assert ta.attn_paged_workspace_bytes(32, 8, 128, 64) == 64 * 2 * 4 * 130 * 4
+    assert ta.attn_paged_workspace_bytes(5, 1, 64, 3) == 3 * 2 * 8 * 66 * 4       # rows in fours
+    assert ta.attn_paged_workspace_bytes(48, 1, 64, 1) == 2 * 24 * 66 * 4         # two row blocks of 24
+    assert ta.attn_paged_workspace_bytes(32, 8, 128, 0) == 0
+    for bad in [(32, 5, 128, 4), (0, 1, 64, 4), (32, 8, 96, 4), (32, 8, 128, -1), (32, 8, 128, 4097)]:
+        with pytest.raises(ta.TileAttnError):
+            ta.attn_paged_workspace_bytes(*bad)
+    for B in (1, 7, 64, 1000):
+        for Hq, Hkv in ((1, 1), (32, 8), (64, 1)):
+            for cap in (1, 100, 10000, 1 << 24):
+                assert 0 <= ta.attn_paged_plan(B, Hq, Hkv, 128, 16, cap) <= 4096
+    for bad in [(0, 1, 1, 64, 16, 1), (1, 3, 2, 64, 16, 1), (1, 1, 1, 32, 16, 1), (1, 1, 1, 64, 0, 1), (1, 1, 1, 64, 16, 0)]:
+        with pytest.raises(ta.TileAttnError):
+            ta.attn_paged_plan(*bad)
 
 
 A, B, BIAS, R, C = (0x100000000 * i for i in range(1, 6))

@@ -129,9 +129,13 @@ def test_attention_against_oracle(ta, case, dtype):
     q = torch.randn(len(lens), Hq + 3, D, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()[:, 1:Hq + 1]
     o = torch.full((len(lens), Hq, D), float("nan"), dtype=dtype, device="cuda")
     lse = torch.full((len(lens), Hq), float("nan"), device="cuda")
-    r = ta.attn_decode_paged(q, *c.args(), **c.scales(), out=o, lse=lse, out_dtype=dtype)
-    assert r[0] is o and r[1] is lse
-    check(c, o, lse, reference(q, c, D ** -0.5))
+    ref = reference(q, c, D ** -0.5)
+    for parts in (None, 0, 1, 3, 37, 512):
+        print(f"  parts {parts}", flush=True)
+        o.fill_(float("nan")), lse.fill_(float("nan"))
+        r = ta.attn_decode_paged(q, *c.args(), **c.scales(), out=o, lse=lse, num_parts=parts, out_dtype=dtype)
+        assert r[0] is o and r[1] is lse
+        check(c, o, lse, ref)
 
 
 @pytest.mark.parametrize("scale", [0.0, 1.0, 40.0])
@@ -139,7 +143,8 @@ def test_attention_scales(ta, scale):
     """Equal weights, and softmaxes that are all but one-hot."""
     c = Cache([200, 33, 1], 2, 64, 16, seed=5)
     q = torch.randn(3, 6, 64, generator=torch.Generator().manual_seed(2)).to(BF16).cuda()
-    check(c, *ta.attn_decode_paged(q, *c.args(), scale=scale), reference(q, c, scale))
+    for parts in (0, 2):
+        check(c, *ta.attn_decode_paged(q, *c.args(), scale=scale, num_parts=parts), reference(q, c, scale))
 
 
 def test_attention_of_bad_lengths_and_pages(ta):
@@ -152,7 +157,8 @@ def test_attention_of_bad_lengths_and_pages(ta):
     c.table[3, 3], c.table[4, 0] = -7, c.k.shape[0]
     ref = reference(q, c, 0.1)
     assert np.isnan(ref[1][1:5]).all() and np.isfinite(ref[1][[0, 5, 6]]).all()
-    check(c, *ta.attn_decode_paged(q, *c.args(), scale=0.1), ref)
+    for parts in (None, 0, 1, 5, 64):
+        check(c, *ta.attn_decode_paged(q, *c.args(), scale=0.1, num_parts=parts), ref)
 
 
 def test_sequences_that_share_pages(ta):
