@@ -106,6 +106,7 @@ struct PagedArgs {
 constexpr int NW = PAGED_NW;
 constexpr float LN2 = 0.69314718055994530942f;
 constexpr float RESCALE_SLACK = 8.f;
+constexpr int DPP_ROR8 = 0x128;   // lanes rotated by eight within rows of sixteen
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c)
 {
@@ -140,28 +141,39 @@ __device__ __forceinline__ uint32_t e4m3_bf16(uint32_t w)
 __device__ __forceinline__ uint32_t high16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302); }
 __device__ __forceinline__ uint32_t low16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100); }
 
-// The batch's tiles, and the sequence that tile t (of all) lies in: every wave
-// finds both by itself from the lengths.  HR: K/V heads times row blocks.
+// The batch's tiles, and the sequence that tile t of a share lies in: every wave
+// finds both by itself from the lengths, 64 sequences at a time.  HR: K/V heads
+// times row blocks.
 struct Place {
-    uint32_t b, first;   // the sequence, and its first tile
+    uint32_t b, first, per;   // the sequence, its first tile, its tiles of one head
 };
 
-__device__ __forceinline__ uint32_t all_tiles(const PagedArgs &a, uint32_t HR, int cap, int tile, int lane)
+__device__ __forceinline__ uint32_t wave_sum(uint32_t n)
 {
-    uint32_t n = 0;
-    for (int i = lane; i < a.B; i += 64)
-        n += paged_tiles(a.lens[i], cap, tile);
 #pragma unroll
     for (int o = 32; o; o >>= 1)
         n += __shfl_xor(n, o);
-    return __builtin_amdgcn_readfirstlane(n) * HR;
+    return __builtin_amdgcn_readfirstlane(n);
 }
 
-__device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int cap, int tile, int lane, uint32_t t)
+__device__ __forceinline__ uint32_t tiles_at(const PagedArgs &a, int cap, int i)
+{
+    return i < a.B ? paged_tiles(a.lens[i], cap) : 0;
+}
+
+__device__ __forceinline__ uint32_t all_tiles(const PagedArgs &a, uint32_t HR, int cap, int lane)
+{
+    uint32_t n = 0;
+    for (int i = lane; i < a.B; i += 64)
+        n += tiles_at(a, cap, i);
+    return wave_sum(n) * HR;
+}
+
+// n: the tiles of sequence `lane` (tiles_at(lane))
+__device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int cap, int lane, uint32_t n, uint32_t t)
 {
     uint32_t base = 0;
-    for (int i0 = 0; i0 < a.B; i0 += 64) {
-        const uint32_t n = i0 + lane < a.B ? paged_tiles(a.lens[i0 + lane], cap, tile) : 0;
+    for (int i0 = 0;; i0 += 64) {
         uint32_t s = n;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -169,14 +181,14 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
             s += lane >= o ? u : 0;
         }
         const uint64_t after = __builtin_amdgcn_ballot_w64(base + s * HR > t);   // sequences that end past t
-        if (after) {
-            const int l = __builtin_ctzll(after);
+        if (after || i0 + 64 >= a.B) {   // (t is one of the tiles: never the second)
+            const int l = after ? __builtin_ctzll(after) : 0;
             const uint32_t end = __builtin_amdgcn_readlane(s, l), own = __builtin_amdgcn_readlane(n, l);
-            return {(uint32_t)(i0 + l), base + (end - own) * HR};
+            return {(uint32_t)(i0 + l), base + (end - own) * HR, own};
         }
         base += __builtin_amdgcn_readlane(s, 63) * HR;
+        n = tiles_at(a, cap, i0 + 64 + lane);
     }
-    return {0, 0};   // (t is one of the tiles)
 }
 
 // Attention of one new token per sequence.  HBM bounds it: every key and value is
@@ -192,19 +204,20 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 //    sums; the next K is loaded under the softmax and the product with V, the
 //    next V under the scores.  The NW waves of a workgroup meet in LDS at the end
 //    of a head's keys.
-//  * The positions of the whole batch, head by head, are one list of tiles of NW
-//    steps; each workgroup takes an even share of it (parts), so a batch of mixed
+//  * The positions of the whole batch, head by head, are one list of tiles of 16
+//    keys per wave; each workgroup takes an even share of it (parts), so a batch of mixed
 //    lengths occupies the GPU as one of equal ones does, without the host knowing
 //    the lengths.  Heads that a share's ends cut leave partial results for
 //    attn_paged_merge_kernel.
 //  * A 16-key block lies in one page (page_size >= 16), so pages are looked up in
 //    scalar registers, a step ahead.
 template <int D, bool E4M3, int RT>
-__global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
+__global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
-    constexpr int KS = paged_step(D, E4M3);      // keys per wave and step
-    constexpr int KB = KS / 16;                  // blocks of 16 keys
-    constexpr int TILE = KS * NW;
+    // 16-key blocks per step: 16 KB of K and V, 8 KB where rows are 64 bytes or
+    // where twice the rows' sums leave no registers for more
+    constexpr int KB = D == 128 && (!E4M3 || RT == 2) ? 2 : 4;
+    constexpr int KS = 16 * KB;
     constexpr int KK = D / 32;                   // k-steps of the scores
     constexpr int ROW = D * (E4M3 ? 1 : 2);      // bytes of a key
     constexpr int KL = ROW / 64;                 // 16-byte loads per lane and key block
@@ -223,16 +236,17 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
     // block) of sequence b, `left` of them
     uint32_t b, hr, t, left;
     if (a.parts) {
-        const uint32_t n = all_tiles(a, HR, cap, TILE, lane), used = paged_parts_used(n, a.parts);
+        const uint32_t mine = tiles_at(a, cap, lane);
+        const uint32_t n = a.B <= 64 ? wave_sum(mine) * HR : all_tiles(a, HR, cap, lane);
+        const uint32_t used = paged_parts_used(n, a.parts);
         if (blockIdx.x >= used)
             return;
         const uint32_t begin = paged_part_begin(n, used, blockIdx.x);
         left = paged_part_begin(n, used, blockIdx.x + 1) - begin;
-        const Place at = place_of(a, HR, cap, TILE, lane, begin);
-        const uint32_t per = paged_tiles(a.lens[at.b], cap, TILE);
+        const Place at = place_of(a, HR, cap, lane, mine, begin);
         b = at.b;
-        hr = (begin - at.first) / per;
-        t = (begin - at.first) % per;
+        hr = (begin - at.first) / at.per;
+        t = (begin - at.first) % at.per;
     } else {
         b = blockIdx.x / HR;
         hr = blockIdx.x % HR;
@@ -243,14 +257,16 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
     for (;;) {
         const int len = __builtin_amdgcn_readfirstlane(a.lens[b]);
         const bool bad_len = len < 0 || len > cap;
-        const uint32_t per = paged_tiles(len, cap, TILE);
+        const uint32_t per = paged_tiles(len, cap);
         const uint32_t take = min(left, per - t);
         const int h = hr / a.blocks, r0 = (hr % a.blocks) * a.rows;
         const int rows = min(a.rows, a.group - r0);      // query rows of this block
         const size_t row0 = (size_t)b * a.Hq + (size_t)h * a.group + r0;
-        const int k_lo = t * TILE, k_hi = bad_len ? 0 : min(len, (int)((t + take) * TILE));
-        const int first = k_lo + wave * KS;
-        const int steps = first < k_hi ? (k_hi - first + TILE - 1) / TILE : 0;
+        const int k_lo = paged_key(t), end = bad_len ? 0 : min(len, paged_key(t + take));
+        // this wave's keys: its share of the blocks, as even as they go
+        const int nb = max(end - k_lo + 15, 0) >> 4;
+        const int first = k_lo + 16 * (nb * wave / NW), k_hi = min(end, k_lo + 16 * (nb * (wave + 1) / NW));
+        const int steps = first < k_hi ? (k_hi - first + KS - 1) / KS : 0;
         const int *const table = a.table + (size_t)b * a.max_pages;
 
         // Q as the B operand: row c16, the dims of the lane's K loads (rows past
@@ -283,12 +299,12 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
         auto lookup = [&](int s, int (&page)[KB]) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const int blk = min(((first + s * TILE) >> 4) + kb, last_block);
+                const int blk = min(((first + s * KS) >> 4) + kb, last_block);
                 page[kb] = paged_checked(table[blk >> (a.page_shift - 4)], a.num_pages);
             }
         };
         auto block_at = [&](int s, int kb, int page) {
-            const int blk = min(((first + s * TILE) >> 4) + kb, last_block);
+            const int blk = min(((first + s * KS) >> 4) + kb, last_block);
             const int in = (blk << 4) & ((1 << a.page_shift) - 1);
             return (((size_t)max(page, 0) * a.Hkv + h) << a.page_shift) * ROW + (size_t)in * ROW;
         };
@@ -298,9 +314,14 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const unsigned char *p = (const unsigned char *)a.K + block_at(s, kb, page[kb]);
+                if constexpr (KL == 1) {
+                    kr[kb][0] = __builtin_nontemporal_load((const u32x4 *)(p + (uint32_t)(c16 * ROW + 16 * g)));
+                } else {
 #pragma unroll
-                for (int i = 0; i < KL; ++i)
-                    kr[kb][i] = *(const u32x4 *)(p + (uint32_t)(c16 * ROW + 64 * i + 16 * g));
+                    for (int i = 0; i < KL; ++i)   // row 8 (i & 1) + c16 % 8, 16-byte chunk g + 4 (c16 / 8) of line i / 2
+                        kr[kb][i] = __builtin_nontemporal_load((const u32x4 *)(
+                            p + (uint32_t)((8 * (i & 1) + (c16 & 7)) * ROW + 128 * (i >> 1) + 64 * (c16 >> 3) + 16 * g)));
+                }
             }
         };
         auto load_v = [&](int s, const int (&page)[KB]) {
@@ -311,16 +332,16 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
                 for (int i = 0; i < 4; ++i) {
                     const unsigned char *e = p + (uint32_t)((4 * g + i) * ROW + c16 * (4 * VW));
                     if constexpr (VW == 4) {
-                        const u32x4 x = *(const u32x4 *)e;
+                        const u32x4 x = __builtin_nontemporal_load((const u32x4 *)e);
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
                             vr[kb][i][w] = x[w];
                     } else if constexpr (VW == 2) {
-                        const u32x2 x = *(const u32x2 *)e;
+                        const u32x2 x = __builtin_nontemporal_load((const u32x2 *)e);
                         vr[kb][i][0] = x[0];
                         vr[kb][i][1] = x[1];
                     } else {
-                        vr[kb][i][0] = *(const uint32_t *)e;
+                        vr[kb][i][0] = __builtin_nontemporal_load((const uint32_t *)e);
                     }
                 }
             }
@@ -335,8 +356,23 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
                 lookup(1, next);
         }
         for (int s = 0; s < steps; ++s) {
-            const int key0 = first + s * TILE;
+            const int key0 = first + s * KS;
             const bool tail = key0 + KS > k_hi;      // uniform
+            // The K loads took whole lines of eight rows each (halves of sixteen rows'
+            // lines would come from HBM twice); lanes c16 and c16 ^ 8 exchange what the
+            // other's row needs: then lane c16 holds chunks 8 l + g and 8 l + 4 + g of row c16
+            if constexpr (KL > 1) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < KL; i += 2)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int x = kr[kb][i][w], y = kr[kb][i + 1][w];
+                            kr[kb][i][w] = __builtin_amdgcn_update_dpp(x, y, DPP_ROR8, 0xF, 0xC, false);
+                            kr[kb][i + 1][w] = __builtin_amdgcn_update_dpp(y, x, DPP_ROR8, 0xF, 0x3, false);
+                        }
+            }
             // scores: lane holds keys 16 kb + 4 g + r of row c16
             f32x4 sc[RT][KB];
 #pragma unroll
@@ -547,21 +583,23 @@ __global__ __launch_bounds__(64 * NW) void attn_paged_kernel(PagedArgs a)
     }
 }
 
-// Joins the partial results of the heads that were cut: a workgroup per
-// (sequence, K/V head, row block), its threads in groups that take every
-// n-th record, then in LDS.
-constexpr int MERGE_T = 512;
+// Joins the partial results of the heads that were cut: a workgroup per m_rows
+// query rows of a (sequence, K/V head, row block), several threads per 16 bytes
+// of them that take every n-th record each, U at a time, and meet in LDS.  It is
+// a chain of latencies, so rows get workgroups of their own while there are few.
+constexpr int MERGE_T = 256;
 template <int D>
-__global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, int tile)
+__global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, int m_rows)
 {
     __shared__ __attribute__((aligned(16))) float so[MERGE_T][4];
     __shared__ float sm[MERGE_T], sl[MERGE_T];
     const int tid = threadIdx.x, lane = tid & 63;
     const int cap = a.max_pages << a.page_shift;
-    const uint32_t HR = a.Hkv * a.blocks, b = blockIdx.x / HR, hr = blockIdx.x % HR;
+    const uint32_t HR = a.Hkv * a.blocks, subs = (a.rows + m_rows - 1) / m_rows;
+    const uint32_t b = blockIdx.x / subs / HR, hr = blockIdx.x / subs % HR;
     uint32_t n = 0, before = 0;   // tiles of the batch, and of the sequences before b
     for (int i = lane; i < a.B; i += 64) {
-        const uint32_t x = paged_tiles(a.lens[i], cap, tile);
+        const uint32_t x = paged_tiles(a.lens[i], cap);
         n += x;
         before += (uint32_t)i < b ? x : 0;
     }
@@ -571,14 +609,19 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
         before += __shfl_xor(before, o);
     }
     n = __builtin_amdgcn_readfirstlane(n) * HR;
-    const uint32_t per = paged_tiles(a.lens[b], cap, tile);
+    const int len = __builtin_amdgcn_readfirstlane(a.lens[b]);
+    const bool bad_len = len < 0 || len > cap;
+    const uint32_t per = paged_tiles(len, cap);
     const uint32_t t0 = __builtin_amdgcn_readfirstlane(before) * HR + hr * per;
     const uint32_t used = paged_parts_used(n, a.parts);
     const uint32_t p0 = paged_part_of(n, used, t0), p1 = paged_part_of(n, used, t0 + per - 1);
     if (p0 == p1)
         return;   // a head that one workgroup took whole
     const int h = hr / a.blocks, r0 = (hr % a.blocks) * a.rows;
-    const int rows = min(a.rows, a.group - r0);
+    const int x0 = blockIdx.x % subs * m_rows;   // the first of these rows in the block
+    const int rows = min(m_rows, min(a.rows, a.group - r0) - x0);
+    if (rows <= 0)
+        return;
     const size_t row0 = (size_t)b * a.Hq + (size_t)h * a.group + r0;
     const size_t pad = (size_t)(a.rows + 3) & ~3, rec = paged_record(a.rows, D);
     const float vs = a.vs ? a.vs[h] : 1.f;
@@ -592,10 +635,10 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
     const int k = tid / width;
     for (int e0 = 0; e0 < items; e0 += width) {
         const int e = e0 + tid % width;
-        const int x = min(e, items - 1) / (D / 4), ch = min(e, items - 1) % (D / 4);
+        const int x = x0 + min(e, items - 1) / (D / 4), ch = min(e, items - 1) % (D / 4);
         float m = -INFINITY, l = 0.f;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        constexpr int U = 4;                     // records in flight
+        constexpr int U = 8;                     // records in flight
         for (uint32_t p = p0 + k; p <= p1; p += U * per_item) {
             float mp[U], lp[U];
             f32x4 op[U];
@@ -634,14 +677,14 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
                 l = l * f0 + sl[s] * f1;
                 o = o * f0 + *(const f32x4 *)so[s] * f1;
             }
-            o *= l == 0.f ? 0.f : vs / l;
+            o *= bad_len ? NAN : l == 0.f ? 0.f : vs / l;
             const size_t at = (row0 + x) * D + 4 * ch;
             if (a.o_bf16)
                 *(u32x2 *)((uint16_t *)a.O + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
             else
                 *(f32x4 *)((float *)a.O + at) = o;
             if (ch == 0)
-                a.LSE[row0 + x] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
+                a.LSE[row0 + x] = bad_len ? NAN : l == 0.f ? -INFINITY : (m + log2f(l)) * LN2;
         }
     }
 }
@@ -752,8 +795,7 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
         num_parts > PAGED_MAX_PARTS)
         return TA_ERR_INVALID_SHAPE;
     const int group = Hq / Hkv, blocks = paged_row_blocks(group);
-    const int tile = paged_step(D, cache_e4m3) * PAGED_NW;
-    if (((int64_t)max_pages * page_size / tile + 1) * B * Hkv * blocks >= 1ll << 31)   // tiles in 32 bits
+    if (((int64_t)max_pages * page_size / PAGED_TILE + 1 + PAGED_HEAD) * B * Hkv * blocks >= 1ll << 31)   // tiles in 32 bits
         return TA_ERR_INVALID_SHAPE;
     if (misaligned(Q) || misaligned(K_cache) || misaligned(V_cache) || misaligned(O) || misaligned(LSE) ||
         misaligned(page_table, 4) || misaligned(seq_lens, 4) || misaligned(k_scale, 4) || misaligned(v_scale, 4))
@@ -798,7 +840,8 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && num_parts) {
         const auto merge = D == 64 ? attn_paged_merge_kernel<64> : attn_paged_merge_kernel<128>;
-        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks)), dim3(MERGE_T), 0, s, a, tile);
+        const int m_rows = min(a.rows, max(1, B * Hq / 512)), subs = (a.rows + m_rows - 1) / m_rows;
+        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks * subs)), dim3(MERGE_T), 0, s, a, m_rows);
         e = hipGetLastError();
     }
     return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;

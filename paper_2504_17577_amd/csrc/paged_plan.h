@@ -17,15 +17,24 @@ constexpr int PAGED_NW = 4;            // waves of an attention workgroup
 constexpr int PAGED_MAX_PARTS = 4096;
 constexpr int PAGED_MAX_ROWS = 32;     // query heads of a group that one workgroup takes
 
-// keys of a wave's step: 16 KB of K and V in flight per wave, 8 KB for 64 dims of 8 bits
-PAGED_FN constexpr int paged_step(int D, bool e4m3) { return D == 128 && !e4m3 ? 32 : 64; }
+// Keys of a tile, the unit that the batch is divided in: a 16-key block per wave,
+// the least that a wave reads, so that shares are even to within it.
+constexpr int PAGED_TILE = 16 * PAGED_NW;
 
-// Tiles of one sequence, counted as at least one (a sequence of no positions, or
-// of a length outside 0..cap, has results to be written too).
-PAGED_FN uint32_t paged_tiles(int len, int cap, int tile)
+// What a head costs besides its keys, in tiles: looking it up, the first loads'
+// way, the meeting of the waves.  Short sequences would make the longest shares
+// without it.  These tiles come first and hold no keys.
+constexpr int PAGED_HEAD = 2;
+
+// Tiles of one sequence's head (a length outside 0..cap counts as none: its
+// results are written too)
+PAGED_FN uint32_t paged_tiles(int len, int cap)
 {
-    return len <= 0 || len > cap ? 1u : (uint32_t)(len - 1) / (uint32_t)tile + 1u;
+    return PAGED_HEAD + (len <= 0 || len > cap ? 0u : (uint32_t)(len - 1) / (uint32_t)PAGED_TILE + 1u);
 }
+
+// The first key of tile t of a head
+PAGED_FN int paged_key(uint32_t t) { return t > PAGED_HEAD ? (int)(t - PAGED_HEAD) * PAGED_TILE : 0; }
 
 // n tiles in `parts` parts, as even as they go: the first n % parts get one more
 PAGED_FN uint32_t paged_part_begin(uint32_t n, uint32_t parts, uint32_t p)

@@ -37,23 +37,23 @@ static void check_parts(uint32_t n, uint32_t parts)
 }
 
 /* the kernels' walk: which part writes what of every head */
-static void walk(const int *lens, int B, int cap, int tile, uint32_t HR, uint32_t parts)
+static void walk(const int *lens, int B, int cap, uint32_t HR, uint32_t parts)
 {
     uint32_t n = 0;
     for (int b = 0; b < B; ++b)
-        n += paged_tiles(lens[b], cap, tile);
+        n += paged_tiles(lens[b], cap);
     n *= HR;
     const uint32_t used = paged_parts_used(n, parts);
     const size_t heads = (size_t)B * HR;
     std::vector<int> whole(heads), tiles(heads), record(2 * used, -1);   /* the head of each record */
     for (uint32_t p = 0; p < used; ++p) {
         uint32_t at = paged_part_begin(n, used, p), left = paged_part_begin(n, used, p + 1) - at, b = 0, first = 0;
-        while (first + HR * paged_tiles(lens[b], cap, tile) <= at)
-            first += HR * paged_tiles(lens[b++], cap, tile);
-        uint32_t per = paged_tiles(lens[b], cap, tile), hr = (at - first) / per, t = (at - first) % per;
+        while (first + HR * paged_tiles(lens[b], cap) <= at)
+            first += HR * paged_tiles(lens[b++], cap);
+        uint32_t per = paged_tiles(lens[b], cap), hr = (at - first) / per, t = (at - first) % per;
         for (;;) {
             EXPECT(b < (uint32_t)B && hr < HR, "past the last head");
-            per = paged_tiles(lens[b], cap, tile);
+            per = paged_tiles(lens[b], cap);
             const uint32_t take = left < per - t ? left : per - t;
             const size_t head = (size_t)b * HR + hr;
             tiles[head] += (int)take;
@@ -73,7 +73,7 @@ static void walk(const int *lens, int B, int cap, int tile, uint32_t HR, uint32_
     }
     uint32_t t0 = 0;
     for (size_t head = 0; head < heads; ++head) {       /* the merge */
-        const uint32_t per = paged_tiles(lens[head / HR], cap, tile);
+        const uint32_t per = paged_tiles(lens[head / HR], cap);
         EXPECT(tiles[head] == (int)per, "head %zu: %d tiles of %u", head, tiles[head], per);
         const uint32_t p0 = paged_part_of(n, used, t0), p1 = paged_part_of(n, used, t0 + per - 1);
         EXPECT(whole[head] == (p0 == p1), "head %zu whole", head);
@@ -91,9 +91,13 @@ int main(void)
     for (size_t i = 0; i < sizeof ns / sizeof *ns; ++i)
         for (size_t j = 0; j < sizeof ps / sizeof *ps; ++j)
             check_parts(ns[i], ps[j]);
-    EXPECT(paged_tiles(0, 100, 32) == 1 && paged_tiles(-5, 100, 32) == 1 && paged_tiles(101, 100, 32) == 1, "one tile");
-    EXPECT(paged_tiles(1, 100, 32) == 1 && paged_tiles(32, 100, 32) == 1 && paged_tiles(33, 100, 32) == 2, "tiles");
-    EXPECT(paged_tiles(1 << 30, 1 << 30, 128) == 1 << 23 && paged_tiles(INT32_MIN, 1 << 30, 128) == 1, "largest");
+    const int T = PAGED_TILE, H = PAGED_HEAD;
+    EXPECT(paged_tiles(0, 100) == (uint32_t)H && paged_tiles(-5, 100) == (uint32_t)H && paged_tiles(101, 100) == (uint32_t)H, "no keys");
+    EXPECT(paged_tiles(1, 999) == (uint32_t)H + 1 && paged_tiles(T, 999) == (uint32_t)H + 1 && paged_tiles(T + 1, 999) == (uint32_t)H + 2, "tiles");
+    EXPECT(paged_tiles(1 << 30, 1 << 30) == (1u << 30) / T + H && paged_tiles(INT32_MIN, 1 << 30) == (uint32_t)H, "largest");
+    EXPECT(paged_key(0) == 0 && paged_key(H) == 0 && paged_key(H + 1) == T && paged_key(H + 5) == 5 * T, "keys");
+    for (int len : {1, 2, T - 1, T, T + 1, 1000, (1 << 30) - 1, 1 << 30})
+        EXPECT(paged_key(paged_tiles(len, 1 << 30)) >= len && paged_key(paged_tiles(len, 1 << 30) - 1) < len, "last tile of %d", len);
     EXPECT(paged_checked(0, 1) == 0 && paged_checked(1, 1) == -1 && paged_checked(-1, 1) == -1 &&
                paged_checked(INT32_MIN, 1) == -1 && paged_checked(INT32_MAX, 1 << 28) == -1, "pages");
     for (int g = 1; g <= 300; ++g) {
@@ -107,7 +111,7 @@ int main(void)
         const int B = 1 + rand() % 80, cap = 1 + rand() % 3000;
         for (int b = 0; b < B; ++b)
             lens[b] = rand() % 4 == 0 ? rand() % 3 - 1 : rand() % (cap + 2);
-        walk(lens, B, cap, 64 << rand() % 3, 1 + (uint32_t)(rand() % 9), 1 + (uint32_t)(rand() % 600));
+        walk(lens, B, cap, 1 + (uint32_t)(rand() % 9), 1 + (uint32_t)(rand() % 600));
     }
     if (failures)
         return 1;
