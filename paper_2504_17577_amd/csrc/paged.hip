@@ -103,6 +103,11 @@ struct PagedArgs {
     float c;                   // scale * log2(e)
 };
 
+// Wave-uniform words that the launch only reads, through the scalar cache: their
+// loads are counted apart from the vector loads, which return in order (a page
+// looked up behind the loads of V would wait for all of them)
+typedef const __attribute__((address_space(4))) int scalar_int;
+
 constexpr int NW = PAGED_NW;
 constexpr float LN2 = 0.69314718055994530942f;
 constexpr float RESCALE_SLACK = 8.f;
@@ -141,53 +146,66 @@ __device__ __forceinline__ uint32_t e4m3_bf16(uint32_t w)
 __device__ __forceinline__ uint32_t high16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302); }
 __device__ __forceinline__ uint32_t low16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100); }
 
-// The batch's tiles, and the sequence that tile t of a share lies in: every wave
-// finds both by itself from the lengths, 64 sequences at a time.  HR: K/V heads
-// times row blocks.
-struct Place {
-    uint32_t b, first, per;   // the sequence, its first tile, its tiles of one head
+// Inclusive sums over the wave's lanes, in the vector ALU (rows of sixteen by
+// shifts, then the rows' last lanes broadcast)
+__device__ __forceinline__ uint32_t wave_scan(uint32_t n)
+{
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xF, 0xF, true);    // row_shr:1, 2, 4, 8
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xF, 0xF, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xF, 0xF, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xF, 0xF, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xA, 0xF, false);   // row_bcast:15 to rows 1 and 3
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xC, 0xF, false);   // row_bcast:31 to rows 2 and 3
+    return n;
+}
+
+__device__ __forceinline__ int len_at(const PagedArgs &a, int i) { return i < a.B ? a.lens[i] : 0; }
+
+// The length and tiles of 64 sequences, one a lane, and where their tiles end
+// among the batch's: the kernels find their places from the lengths, 64
+// sequences at a time.
+struct Lengths {
+    int len;
+    uint32_t tiles, ends;
 };
 
-__device__ __forceinline__ uint32_t wave_sum(uint32_t n)
+__device__ __forceinline__ Lengths lengths_at(const PagedArgs &a, int cap, int i)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1)
-        n += __shfl_xor(n, o);
-    return __builtin_amdgcn_readfirstlane(n);
+    const int len = len_at(a, i);
+    const uint32_t n = i < a.B ? paged_tiles(len, cap) : 0;
+    return {len, n, wave_scan(n)};
 }
 
-__device__ __forceinline__ uint32_t tiles_at(const PagedArgs &a, int cap, int i)
+// The batch's tiles of one K/V head and row block, from the first 64 sequences'
+__device__ __forceinline__ uint32_t all_tiles(const PagedArgs &a, int cap, int lane, const Lengths &first)
 {
-    return i < a.B ? paged_tiles(a.lens[i], cap) : 0;
+    uint32_t n = __builtin_amdgcn_readlane(first.ends, 63);
+    for (int i0 = 64; i0 < a.B; i0 += 64)
+        n += __builtin_amdgcn_readlane(lengths_at(a, cap, i0 + lane).ends, 63);
+    return n;
 }
 
-__device__ __forceinline__ uint32_t all_tiles(const PagedArgs &a, uint32_t HR, int cap, int lane)
-{
-    uint32_t n = 0;
-    for (int i = lane; i < a.B; i += 64)
-        n += tiles_at(a, cap, i);
-    return wave_sum(n) * HR;
-}
+// The sequence that tile t lies in, its length, first tile and tiles of a head
+// (HR: K/V heads times row blocks)
+struct Place {
+    uint32_t b;
+    int len;
+    uint32_t first, per;
+};
 
-// n: the tiles of sequence `lane` (tiles_at(lane))
-__device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int cap, int lane, uint32_t n, uint32_t t)
+__device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int cap, int lane, Lengths at, uint32_t t)
 {
     uint32_t base = 0;
     for (int i0 = 0;; i0 += 64) {
-        uint32_t s = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t u = __shfl_up(s, o);
-            s += lane >= o ? u : 0;
-        }
-        const uint64_t after = __builtin_amdgcn_ballot_w64(base + s * HR > t);   // sequences that end past t
+        const uint64_t after = __builtin_amdgcn_ballot_w64((base + at.ends) * HR > t);   // sequences that end past t
         if (after || i0 + 64 >= a.B) {   // (t is one of the tiles: never the second)
             const int l = after ? __builtin_ctzll(after) : 0;
-            const uint32_t end = __builtin_amdgcn_readlane(s, l), own = __builtin_amdgcn_readlane(n, l);
-            return {(uint32_t)(i0 + l), base + (end - own) * HR, own};
+            const uint32_t own = __builtin_amdgcn_readlane(at.tiles, l);
+            return {(uint32_t)(i0 + l), (int)__builtin_amdgcn_readlane(at.len, l),
+                    (base + __builtin_amdgcn_readlane(at.ends, l) - own) * HR, own};
         }
-        base += __builtin_amdgcn_readlane(s, 63) * HR;
-        n = tiles_at(a, cap, i0 + 64 + lane);
+        base += __builtin_amdgcn_readlane(at.ends, 63);
+        at = lengths_at(a, cap, i0 + 64 + lane);
     }
 }
 
@@ -214,9 +232,7 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 template <int D, bool E4M3, int RT>
 __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
-    // 16-key blocks per step: 16 KB of K and V, 8 KB where rows are 64 bytes or
-    // where twice the rows' sums leave no registers for more
-    constexpr int KB = D == 128 && (!E4M3 || RT == 2) ? 2 : 4;
+    constexpr int KB = 2;                        // 16-key blocks per wave and step
     constexpr int KS = 16 * KB;
     constexpr int KK = D / 32;                   // k-steps of the scores
     constexpr int ROW = D * (E4M3 ? 1 : 2);      // bytes of a key
@@ -235,27 +251,29 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
     // the tiles of this workgroup: from tile t of head `hr` (K/V head and row
     // block) of sequence b, `left` of them
     uint32_t b, hr, t, left;
+    int len;
     if (a.parts) {
-        const uint32_t mine = tiles_at(a, cap, lane);
-        const uint32_t n = a.B <= 64 ? wave_sum(mine) * HR : all_tiles(a, HR, cap, lane);
+        const Lengths some = lengths_at(a, cap, lane);
+        const uint32_t n = all_tiles(a, cap, lane, some) * HR;
         const uint32_t used = paged_parts_used(n, a.parts);
         if (blockIdx.x >= used)
             return;
         const uint32_t begin = paged_part_begin(n, used, blockIdx.x);
         left = paged_part_begin(n, used, blockIdx.x + 1) - begin;
-        const Place at = place_of(a, HR, cap, lane, mine, begin);
+        const Place at = place_of(a, HR, cap, lane, some, begin);
         b = at.b;
+        len = at.len;
         hr = (begin - at.first) / at.per;
         t = (begin - at.first) % at.per;
     } else {
         b = blockIdx.x / HR;
         hr = blockIdx.x % HR;
+        len = ((scalar_int *)(uintptr_t)a.lens)[b];
         t = 0;
         left = ~0u;
     }
 
     for (;;) {
-        const int len = __builtin_amdgcn_readfirstlane(a.lens[b]);
         const bool bad_len = len < 0 || len > cap;
         const uint32_t per = paged_tiles(len, cap);
         const uint32_t take = min(left, per - t);
@@ -267,7 +285,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
         const int nb = max(end - k_lo + 15, 0) >> 4;
         const int first = k_lo + 16 * (nb * wave / NW), k_hi = min(end, k_lo + 16 * (nb * (wave + 1) / NW));
         const int steps = first < k_hi ? (k_hi - first + KS - 1) / KS : 0;
-        const int *const table = a.table + (size_t)b * a.max_pages;
+        scalar_int *const table = (scalar_int *)(uintptr_t)(a.table + (size_t)b * a.max_pages);
 
         // Q as the B operand: row c16, the dims of the lane's K loads (rows past
         // the last read the last; they are never stored)
@@ -293,27 +311,33 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // the rows of this head in a step's blocks: from the page's first row,
-        // bytes from the cache's start; a block past the last key is the last one
+        // the pages of a step's blocks, and where the head's rows of the blocks are,
+        // in bytes from the cache's start; a block past the last key is the last one
         const int last_block = (k_hi - 1) >> 4;
-        auto lookup = [&](int s, int (&page)[KB]) {
+        int page[KB];
+        auto lookup = [&](int s) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+                page[kb] = table[min(((first + s * KS) >> 4) + kb, last_block) >> (a.page_shift - 4)];
+        };
+        size_t at[KB];
+        bool bad[KB], next_bad[KB];
+        auto place = [&](int s) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
+                const int pg = paged_checked(page[kb], a.num_pages);
                 const int blk = min(((first + s * KS) >> 4) + kb, last_block);
-                page[kb] = paged_checked(table[blk >> (a.page_shift - 4)], a.num_pages);
+                const int in = (blk << 4) & ((1 << a.page_shift) - 1);
+                at[kb] = ((((size_t)max(pg, 0) * a.Hkv + h) << a.page_shift) + in) * ROW;
+                next_bad[kb] = pg < 0;
             }
-        };
-        auto block_at = [&](int s, int kb, int page) {
-            const int blk = min(((first + s * KS) >> 4) + kb, last_block);
-            const int in = (blk << 4) & ((1 << a.page_shift) - 1);
-            return (((size_t)max(page, 0) * a.Hkv + h) << a.page_shift) * ROW + (size_t)in * ROW;
         };
         u32x4 kr[KB][KL];
         uint32_t vr[KB][4][VW];
-        auto load_k = [&](int s, const int (&page)[KB]) {
+        auto load_k = [&]() {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const unsigned char *p = (const unsigned char *)a.K + block_at(s, kb, page[kb]);
+                const unsigned char *p = (const unsigned char *)a.K + at[kb];
                 if constexpr (KL == 1) {
                     kr[kb][0] = __builtin_nontemporal_load((const u32x4 *)(p + (uint32_t)(c16 * ROW + 16 * g)));
                 } else {
@@ -324,10 +348,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 }
             }
         };
-        auto load_v = [&](int s, const int (&page)[KB]) {
+        auto load_v = [&]() {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const unsigned char *p = (const unsigned char *)a.V + block_at(s, kb, page[kb]);
+                const unsigned char *p = (const unsigned char *)a.V + at[kb];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const unsigned char *e = p + (uint32_t)((4 * g + i) * ROW + c16 * (4 * VW));
@@ -347,13 +371,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             }
         };
 
-        int page[KB], next[KB];
         if (steps > 0) {
-            lookup(0, page);
-            load_k(0, page);
-            load_v(0, page);
+            lookup(0);
+            place(0);
+            load_k();
+            load_v();
             if (steps > 1)
-                lookup(1, next);
+                lookup(1);
         }
         for (int s = 0; s < steps; ++s) {
             const int key0 = first + s * KS;
@@ -393,12 +417,15 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                         sc[i][kb] = mfma(k, q[i][kk], sc[i][kb]);
                     }
                 }
-            bool bad[KB];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-                bad[kb] = page[kb] < 0;
-            if (s + 1 < steps)
-                load_k(s + 1, next);
+                bad[kb] = next_bad[kb];
+            if (s + 1 < steps) {
+                place(s + 1);
+                load_k();
+                if (s + 2 < steps)
+                    lookup(s + 2);
+            }
             // a page outside the pool makes its keys' scores NaN, and so the row
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -505,14 +532,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                     }
                 }
             }
-            if (s + 1 < steps) {
-                load_v(s + 1, next);
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-                    page[kb] = next[kb];
-                if (s + 2 < steps)
-                    lookup(s + 2, next);
-            }
+            if (s + 1 < steps)
+                load_v();
         }
 
         // The waves' sums meet in LDS, in wave order.  Lane: row c16, dims
@@ -578,7 +599,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
         t = 0;
         if (++hr == HR) {
             hr = 0;
-            ++b;
+            len = ((scalar_int *)(uintptr_t)a.lens)[++b];
         }
     }
 }
@@ -587,7 +608,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 // query rows of a (sequence, K/V head, row block), several threads per 16 bytes
 // of them that take every n-th record each, U at a time, and meet in LDS.  It is
 // a chain of latencies, so rows get workgroups of their own while there are few.
-constexpr int MERGE_T = 256;
+constexpr int MERGE_T = 512;
 template <int D>
 __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, int m_rows)
 {
@@ -598,21 +619,19 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
     const uint32_t HR = a.Hkv * a.blocks, subs = (a.rows + m_rows - 1) / m_rows;
     const uint32_t b = blockIdx.x / subs / HR, hr = blockIdx.x / subs % HR;
     uint32_t n = 0, before = 0;   // tiles of the batch, and of the sequences before b
-    for (int i = lane; i < a.B; i += 64) {
-        const uint32_t x = paged_tiles(a.lens[i], cap);
-        n += x;
-        before += (uint32_t)i < b ? x : 0;
+    int len = 0;
+    for (int i0 = 0; i0 < a.B; i0 += 64) {
+        const Lengths some = lengths_at(a, cap, i0 + lane);
+        if (b / 64 == (uint32_t)i0 / 64) {
+            len = __builtin_amdgcn_readlane(some.len, b % 64);
+            before = n + __builtin_amdgcn_readlane(some.ends - some.tiles, b % 64);
+        }
+        n += __builtin_amdgcn_readlane(some.ends, 63);
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        n += __shfl_xor(n, o);
-        before += __shfl_xor(before, o);
-    }
-    n = __builtin_amdgcn_readfirstlane(n) * HR;
-    const int len = __builtin_amdgcn_readfirstlane(a.lens[b]);
+    n *= HR;
     const bool bad_len = len < 0 || len > cap;
     const uint32_t per = paged_tiles(len, cap);
-    const uint32_t t0 = __builtin_amdgcn_readfirstlane(before) * HR + hr * per;
+    const uint32_t t0 = before * HR + hr * per;
     const uint32_t used = paged_parts_used(n, a.parts);
     const uint32_t p0 = paged_part_of(n, used, t0), p1 = paged_part_of(n, used, t0 + per - 1);
     if (p0 == p1)
@@ -629,9 +648,9 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
     const int items = rows * (D / 4);            // 16-byte chunks of the head's rows
     // threads per group of records: a power of two of them work on one chunk
     int per_item = 1;
-    while (per_item < 16 && items * per_item * 2 <= MERGE_T)
+    while (per_item < 16 && items * per_item * 2 <= (int)blockDim.x)
         per_item *= 2;
-    const int width = MERGE_T / per_item;        // chunks at a time
+    const int width = blockDim.x / per_item;        // chunks at a time
     const int k = tid / width;
     for (int e0 = 0; e0 < items; e0 += width) {
         const int e = e0 + tid % width;
@@ -841,7 +860,8 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
     if (e == hipSuccess && num_parts) {
         const auto merge = D == 64 ? attn_paged_merge_kernel<64> : attn_paged_merge_kernel<128>;
         const int m_rows = min(a.rows, max(1, B * Hq / 512)), subs = (a.rows + m_rows - 1) / m_rows;
-        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks * subs)), dim3(MERGE_T), 0, s, a, m_rows);
+        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks * subs)),
+                           dim3(B * Hq <= 128 ? MERGE_T : MERGE_T / 2), 0, s, a, m_rows);
         e = hipGetLastError();
     }
     return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
@@ -867,7 +887,14 @@ ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_
         return TA_ERR_INVALID_SHAPE;
     if (D != 64 && D != 128)
         return TA_ERR_UNSUPPORTED;
-    *num_parts = (int64_t)max_pages * page_size <= 512 ? 0 : 512;
+    // Two workgroups per CU share the batch, unless the longest sequence the table
+    // has room for is short enough for one workgroup a head, which needs no second
+    // kernel.  us, one a head | 512 parts (bf16, 128 dims, 32 query and 8 K/V heads):
+    // B=1 500 keys 8.8 | 10.2, 2000 keys 29 | 11; B=64 to 1000 mixed 24 | 18; but
+    // B=128 (8-bit) to 800 mixed 17 | 23, B=128 16 heads of 64 dims 200 keys 21 | 28.
+    const int64_t cap = (int64_t)max_pages * page_size;
+    const int64_t heads = (int64_t)B * Hkv * paged_row_blocks(Hq / Hkv);
+    *num_parts = cap <= 512 || (cap <= 1024 && heads >= 1024) ? 0 : 512;
     return TA_OK;
 }
 

@@ -27,7 +27,7 @@ static int failures = 0;
 static void check_parts(uint32_t n, uint32_t parts)
 {
     const uint32_t used = paged_parts_used(n, parts);
-    EXPECT(used >= 1 && used <= parts && used <= n, "used %u", used);
+    EXPECT(used >= 1 && used <= parts && used <= n / 2 + n % 2, "used %u", used);
     EXPECT(paged_part_begin(n, used, 0) == 0 && paged_part_begin(n, used, used) == n, "ends of %u in %u", n, used);
     for (uint32_t p = 0; p < used; ++p) {
         const uint32_t b = paged_part_begin(n, used, p), e = paged_part_begin(n, used, p + 1);
