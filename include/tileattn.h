@@ -520,15 +520,31 @@ typedef enum {
  *   C  device, [M, N] row-major: fp32, or bf16 if c_bf16 != 0      written
  *   activation  a ta_activation (else TA_ERR_UNSUPPORTED)
  *   N % 8 == 0 and K % 8 == 0 (else TA_ERR_UNSUPPORTED); N < 2^24, K < 2^22,
- *   M * N < 2^40 and M * K < 2^40 (else TA_ERR_INVALID_SHAPE); pointers 16-byte
- *   aligned; C apart from A, B and bias, and from residual unless it is C
+ *   M <= 2^20, M * N < 2^36 and M * K < 2^40 (else TA_ERR_INVALID_SHAPE);
+ *   pointers 16-byte aligned; C apart from A, B and bias, and from residual
+ *   unless it is C
+ *   num_splits  1..64 (else TA_ERR_INVALID_SHAPE): ranges of K that separate
+ *               workgroups sum; for more than one, each range's fp32 product
+ *               goes to `workspace` (device, 16-byte aligned, at least
+ *               gemm_epilogue_workspace_bytes(...) bytes, owned by the caller, no
+ *               overlap with any other argument; TA_ERR_WORKSPACE if NULL or
+ *               smaller) and a second kernel adds them in range order
  *
  * Sums, bias, activation and residual are fp32; a bf16 C is rounded once, to
  * nearest even.  Ownership, asynchrony and status codes as gemm_bf16.
  */
 ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, const void *residual,
                              void *C, int c_bf16, int activation, int M, int N, int K,
+                             int num_splits, void *workspace, size_t workspace_bytes,
                              void *stream);
+
+/* Workspace bytes gemm_bf16_epilogue needs: num_splits * M * N * 4 for
+ * num_splits > 1, 0 for 1.  No HIP call. */
+ta_status gemm_epilogue_workspace_bytes(int M, int N, int num_splits, size_t *bytes);
+
+/* A split count for gemm_bf16_epilogue: 1 unless the workgroups of one range
+ * would leave CUs without work.  No HIP call. */
+ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits);
 
 /*
  * ta_schedule — host-side tile schedule of attn_fwd, for tests and tools.

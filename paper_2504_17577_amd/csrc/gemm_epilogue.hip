@@ -8,6 +8,10 @@
 
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -16,70 +20,240 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
-__device__ __forceinline__ float bf16_f32(uint16_t w) { return __uint_as_float((uint32_t)w << 16); }
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 struct EArgs {
     const uint16_t *A, *B, *bias;
     const void *R;
     void *C;
+    float *W;        // with more than one K range: their products [n_split][M][N]
     int M, N, K;
+    int n_split;
+    int act, c_bf16;
 };
 
 // The two gelus and silu as x times a sigmoid-like factor in (0, 1): no
 // difference of nearly equal numbers for negative x.
-template <int ACT>
-__device__ __forceinline__ float activated(float x)
+__device__ __forceinline__ f32x4 activated(int act, f32x4 x)
 {
-    if (ACT == TA_ACT_RELU)
-        return x < 0.f ? 0.f : x;
-    if (ACT == TA_ACT_GELU)
-        return 0.5f * x * erfcf(x * -0.70710678118654752440f);
-    if (ACT == TA_ACT_GELU_TANH)
-        return x / (1.f + expf(-1.59576912160573071176f * (x + 0.044715f * x * x * x)));
-    if (ACT == TA_ACT_SILU)
-        return x / (1.f + expf(-x));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float v = x[i];
+        x[i] = act == TA_ACT_RELU   ? (v < 0.f ? 0.f : v)
+               : act == TA_ACT_GELU ? 0.5f * v * erfcf(v * -0.70710678118654752440f)
+               : act == TA_ACT_GELU_TANH
+                   ? v / (1.f + expf(-1.59576912160573071176f * (v + 0.044715f * v * v * v)))
+               : act == TA_ACT_SILU ? v / (1.f + expf(-v))
+                                    : v;
+    }
     return x;
 }
 
-// A thread per element of C, 16 x 16 of them sharing their operands in LDS.
-template <int ACT, bool CBF16>
-__global__ __launch_bounds__(256) void gemm_epilogue_kernel(EArgs a)
+// Four columns of a row of C from their fp32 sums (n a multiple of 4, in range)
+__device__ __forceinline__ void store4(const EArgs &a, int m, int n, f32x4 x)
 {
-    __shared__ float as[16][17], bs[16][17];
-    const int x = threadIdx.x % 16, y = threadIdx.x / 16;
-    const int m = blockIdx.y * 16 + y, n = blockIdx.x * 16 + x;
-    float sum = 0.f;
-    for (int k0 = 0; k0 < a.K; k0 += 16) {
-        as[y][x] = m < a.M && k0 + x < a.K ? bf16_f32(a.A[(size_t)m * a.K + k0 + x]) : 0.f;
-        bs[y][x] = n < a.N && k0 + y < a.K ? bf16_f32(a.B[(size_t)(k0 + y) * a.N + n]) : 0.f;
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 16; ++k)
-            sum = __builtin_fmaf(as[y][k], bs[k][x], sum);
-        __syncthreads();
-    }
-    if (m >= a.M || n >= a.N)
-        return;
     const size_t e = (size_t)m * a.N + n;
-    if (a.bias)
-        sum += bf16_f32(a.bias[n]);
-    sum = activated<ACT>(sum);
-    if (a.R)
-        sum += CBF16 ? bf16_f32(((const uint16_t *)a.R)[e]) : ((const float *)a.R)[e];
-    if (CBF16)
-        ((uint16_t *)a.C)[e] = (uint16_t)pack_bf16(sum, 0.f);
-    else
-        ((float *)a.C)[e] = sum;
+    if (a.bias) {
+        const u32x2 b = *(const u32x2 *)(a.bias + n);
+        x += f32x4{bf16_lo(b[0]), bf16_hi(b[0]), bf16_lo(b[1]), bf16_hi(b[1])};
+    }
+    x = activated(a.act, x);
+    if (a.c_bf16) {
+        if (a.R) {
+            const u32x2 r = *(const u32x2 *)((const uint16_t *)a.R + e);
+            x += f32x4{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])};
+        }
+        *(u32x2 *)((uint16_t *)a.C + e) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    } else {
+        if (a.R)
+            x += *(const f32x4 *)((const float *)a.R + e);
+        *(f32x4 *)((float *)a.C + e) = x;
+    }
 }
 
-template <int ACT>
-hipError_t launch(const EArgs &a, bool c_bf16, hipStream_t s)
+// ---- few rows: up to 64, a decode step's tokens ---------------------------
+// HBM bounds it: every weight is read once and meets a few tokens.  A wave takes
+// a strip of 128 columns and a range of K: a lane loads the same 8 columns of 8
+// rows (16 bytes each, four whole 256-byte row pieces an instruction) and
+// transposes the 8 x 8 block with byte permutes into the operands of
+// v_mfma_f32_16x16x32_bf16, of which operand j is columns 8 c16 + j: nothing of B
+// goes through LDS.  A's operands are 16 bytes of a row as they are, from L2.
+// C^T = B^T A^T, so that a lane ends up with 32 consecutive columns of a token.
+// The waves of a workgroup take ranges of K of their own and add up in LDS, in
+// wave order; with few strips, workgroups take ranges too (n_split).
+constexpr int SK_WAVES = 8;
+constexpr int SK_COLS = 128;
+
+__device__ __forceinline__ uint32_t high16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302); }
+__device__ __forceinline__ uint32_t low16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100); }
+
+template <bool NT>
+__device__ __forceinline__ u32x4 ld_b(const uint16_t *p)
 {
-    const dim3 grid((a.N + 15) / 16, (a.M + 15) / 16);
-    if (c_bf16)
-        hipLaunchKernelGGL((gemm_epilogue_kernel<ACT, true>), grid, dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((gemm_epilogue_kernel<ACT, false>), grid, dim3(256), 0, s, a);
+    if (NT)
+        return __builtin_nontemporal_load((const u32x4 *)p);
+    return *(const u32x4 *)p;
+}
+
+// MT: blocks of 16 rows.  SPLIT: to the workspace instead of C
+template <int MT, bool SPLIT, bool NT>
+__global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
+{
+    __shared__ __attribute__((aligned(16))) float red[SK_WAVES][16][SK_COLS];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c16 = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * SK_COLS, m0 = blockIdx.z * (16 * MT);
+    const int rows = min(a.M - m0, 16 * MT);
+
+    // this wave's steps of 32 rows of B
+    const int all = (a.K + 31) / 32, parts = gridDim.y * SK_WAVES, part = blockIdx.y * SK_WAVES + wave;
+    const int s0 = (int)((int64_t)all * part / parts), s1 = (int)((int64_t)all * (part + 1) / parts);
+
+    // (columns past N read the last eight, rows past M the last: never stored)
+    const uint16_t *const bp = a.B + min(n0 + 8 * c16, a.N - 8);
+    const uint16_t *const ap = a.A + (size_t)m0 * a.K;
+    uint32_t ao[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        ao[t] = (uint32_t)min(16 * t + c16, rows - 1) * a.K;
+
+    f32x4 acc[MT][8];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    struct Step {
+        u32x4 b[8], x[MT];
+    };
+    auto load = [&](int s, Step &st) {
+        const int k = 32 * s + 8 * g;
+        // (a last step of fewer rows: the lanes behind them read the last eight,
+        // and take zeros below)
+        const int kc = min(k, a.K - 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            st.b[i] = ld_b<NT>(bp + (size_t)(kc + i) * a.N);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            st.x[t] = *(const u32x4 *)(ap + ao[t] + kc);
+    };
+    auto compute = [&](int s, Step &st) {
+        if (32 * s + 32 > a.K) {
+            const bool in = 32 * s + 8 * g < a.K;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    st.b[i][w] = in ? st.b[i][w] : 0u;
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    st.x[t][w] = in ? st.x[t][w] : 0u;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            u32x4 v;
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                v[p] = j & 1 ? high16(st.b[2 * p][j >> 1], st.b[2 * p + 1][j >> 1])
+                             : low16(st.b[2 * p][j >> 1], st.b[2 * p + 1][j >> 1]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
+                                                                    __builtin_bit_cast(bf16x8, st.x[t]), acc[t][j], 0, 0, 0);
+        }
+    };
+    Step st[2];
+    if (s0 < s1)
+        load(s0, st[0]);
+    for (int s = s0; s < s1; s += 2) {
+        if (s + 1 < s1)
+            load(s + 1, st[1]);
+        compute(s, st[0]);
+        if (s + 2 < s1)
+            load(s + 2, st[0]);
+        if (s + 1 < s1)
+            compute(s + 1, st[1]);
+    }
+
+    // lane: row c16 of the block, columns 32 g + 8 r + j; 16-byte chunk ch of row x
+    // at ch ^ x
+    const size_t w0 = SPLIT ? (size_t)blockIdx.y * a.M * a.N : 0;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        if (t)
+            __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                *(f32x4 *)&red[wave][c16][4 * ((8 * g + 2 * r + q) ^ c16)] =
+                    f32x4{acc[t][4 * q][r], acc[t][4 * q + 1][r], acc[t][4 * q + 2][r], acc[t][4 * q + 3][r]};
+        __syncthreads();
+        static_assert(16 * SK_COLS / 4 == 64 * SK_WAVES, "four columns of a row per thread");
+        const int x = tid / (SK_COLS / 4), ch = tid % (SK_COLS / 4);
+        const int m = m0 + 16 * t + x, n = n0 + 4 * ch;
+        if (m < a.M && n < a.N) {
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < SK_WAVES; ++w)
+                sum += *(const f32x4 *)&red[w][x][4 * (ch ^ x)];
+            if (SPLIT)
+                *(f32x4 *)(a.W + w0 + (size_t)m * a.N + n) = sum;
+            else
+                store4(a, m, n, sum);
+        }
+    }
+}
+
+// The ranges' products added in range order, and the epilogue: four columns per
+// thread, up to eight ranges' loads in flight.
+__global__ __launch_bounds__(256) void gemm_join_kernel(EArgs a)
+{
+    const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, mn = (size_t)a.M * a.N;
+    if (e >= mn)
+        return;
+    f32x4 sum = *(const f32x4 *)(a.W + e);
+    for (int s = 1; s < a.n_split; s += 8) {
+        f32x4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = s + u < a.n_split ? *(const f32x4 *)(a.W + (s + u) * mn + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (s + u < a.n_split)
+                sum += v[u];
+    }
+    store4(a, (int)(e / a.N), (int)(e % a.N), sum);
+}
+
+constexpr int MAX_SPLITS = 64;
+
+template <int MT>
+hipError_t launch_few(const EArgs &a, bool nt, hipStream_t s)
+{
+    const dim3 grid((a.N + SK_COLS - 1) / SK_COLS, a.n_split, (a.M + 16 * MT - 1) / (16 * MT)), block(64 * SK_WAVES);
+    const auto kernel = a.n_split > 1 ? (nt ? gemm_few_kernel<MT, true, true> : gemm_few_kernel<MT, true, false>)
+                                      : (nt ? gemm_few_kernel<MT, false, true> : gemm_few_kernel<MT, false, false>);
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch(const EArgs &a, hipStream_t s)
+{
+    const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
+    hipError_t e = a.M <= 16   ? launch_few<1>(a, nt, s)
+                   : a.M <= 32 ? launch_few<2>(a, nt, s)
+                   : a.M <= 48 ? launch_few<3>(a, nt, s)
+                               : launch_few<4>(a, nt, s);
+    if (e != hipSuccess || a.n_split == 1)
+        return e;
+    const size_t threads = (size_t)a.M * a.N / 4;
+    hipLaunchKernelGGL(gemm_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -91,37 +265,81 @@ bool overlaps(const void *p, size_t pn, const void *q, size_t qn)
     return p && q && x < y + qn && y < x + pn;
 }
 
+// the sizes that every entry point checks alike
+ta_status check_sizes(int M, int N, int K)
+{
+    if (M < 1 || N < 1 || K < 1)
+        return TA_ERR_INVALID_SHAPE;
+    if (N % 8 || K % 8)
+        return TA_ERR_UNSUPPORTED;
+    if (N >= 1 << 24 || K >= 1 << 22 || M > 1 << 20 || (int64_t)M * N >= 1ll << 36 || (int64_t)M * K >= 1ll << 40)
+        return TA_ERR_INVALID_SHAPE;
+    return TA_OK;
+}
+
 }  // namespace
 
 extern "C" {
 
 ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, const void *residual,
                              void *C, int c_bf16, int activation, int M, int N, int K,
-                             void *stream)
+                             int num_splits, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!A || !B || !C)
         return TA_ERR_NULL_POINTER;
-    if (M < 1 || N < 1 || K < 1)
+    const ta_status rc = check_sizes(M, N, K);
+    if (rc != TA_OK)
+        return rc;
+    if (num_splits < 1 || num_splits > MAX_SPLITS)
         return TA_ERR_INVALID_SHAPE;
-    if (N % 8 || K % 8 || activation < TA_ACT_NONE || activation > TA_ACT_SILU)
+    if (activation < TA_ACT_NONE || activation > TA_ACT_SILU)
         return TA_ERR_UNSUPPORTED;
-    if (N >= 1 << 24 || K >= 1 << 22 || M > 1 << 20 || (int64_t)M * N >= 1ll << 40 || (int64_t)M * K >= 1ll << 40)
-        return TA_ERR_INVALID_SHAPE;
     if (misaligned(A) || misaligned(B) || misaligned(C) || misaligned(bias) || misaligned(residual))
         return TA_ERR_MISALIGNED;
+    const size_t a_bytes = (size_t)M * K * 2, b_bytes = (size_t)K * N * 2;
     const size_t c_bytes = (size_t)M * N * (c_bf16 ? 2 : 4);
-    if (overlaps(C, c_bytes, A, (size_t)M * K * 2) || overlaps(C, c_bytes, B, (size_t)K * N * 2) ||
+    if (overlaps(C, c_bytes, A, a_bytes) || overlaps(C, c_bytes, B, b_bytes) ||
         overlaps(C, c_bytes, bias, (size_t)N * 2) || (residual != C && overlaps(C, c_bytes, residual, c_bytes)))
         return TA_ERR_ALIASING;
-    const EArgs a = {(const uint16_t *)A, (const uint16_t *)B, (const uint16_t *)bias, residual, C, M, N, K};
-    hipStream_t s = (hipStream_t)stream;
-    const bool cb = c_bf16 != 0;
-    const hipError_t e = activation == TA_ACT_NONE        ? launch<TA_ACT_NONE>(a, cb, s)
-                         : activation == TA_ACT_RELU      ? launch<TA_ACT_RELU>(a, cb, s)
-                         : activation == TA_ACT_GELU      ? launch<TA_ACT_GELU>(a, cb, s)
-                         : activation == TA_ACT_GELU_TANH ? launch<TA_ACT_GELU_TANH>(a, cb, s)
-                                                          : launch<TA_ACT_SILU>(a, cb, s);
-    return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+    if (num_splits > 1) {
+        const size_t w_bytes = (size_t)num_splits * M * N * 4;
+        if (!workspace || workspace_bytes < w_bytes)
+            return TA_ERR_WORKSPACE;
+        if (misaligned(workspace))
+            return TA_ERR_MISALIGNED;
+        if (overlaps(workspace, w_bytes, A, a_bytes) || overlaps(workspace, w_bytes, B, b_bytes) ||
+            overlaps(workspace, w_bytes, C, c_bytes) || overlaps(workspace, w_bytes, bias, (size_t)N * 2) ||
+            overlaps(workspace, w_bytes, residual, c_bytes))
+            return TA_ERR_ALIASING;
+    }
+    const EArgs a = {(const uint16_t *)A, (const uint16_t *)B, (const uint16_t *)bias, residual, C,
+                     (float *)workspace, M, N, K, num_splits, activation, c_bf16 != 0};
+    return launch(a, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+}
+
+ta_status gemm_epilogue_workspace_bytes(int M, int N, int num_splits, size_t *bytes)
+{
+    if (!bytes)
+        return TA_ERR_NULL_POINTER;
+    if (M < 1 || N < 1 || num_splits < 1 || num_splits > MAX_SPLITS)
+        return TA_ERR_INVALID_SHAPE;
+    *bytes = num_splits > 1 ? (size_t)num_splits * M * N * 4 : 0;
+    return TA_OK;
+}
+
+ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
+{
+    if (!num_splits)
+        return TA_ERR_NULL_POINTER;
+    const ta_status rc = check_sizes(M, N, K);
+    if (rc != TA_OK)
+        return rc;
+    const int strips = (N + SK_COLS - 1) / SK_COLS;
+    int sp = 1;
+    while (sp < 16 && strips * sp < 256 && K / (sp * 2 * SK_WAVES) >= 32)
+        sp *= 2;
+    *num_splits = sp;
+    return TA_OK;
 }
 
 }  // extern "C"

@@ -114,7 +114,11 @@ def lib():
     L.attn_paged_plan.restype = i
     L.attn_paged_plan.argtypes = [i] * 6 + [ctypes.POINTER(i)]
     L.gemm_bf16_epilogue.restype = i
-    L.gemm_bf16_epilogue.argtypes = [p] * 5 + [i] * 5 + [p]
+    L.gemm_bf16_epilogue.argtypes = [p] * 5 + [i] * 6 + [p, ctypes.c_size_t, p]
+    L.gemm_epilogue_workspace_bytes.restype = i
+    L.gemm_epilogue_workspace_bytes.argtypes = [i, i, i, ctypes.POINTER(ctypes.c_size_t)]
+    L.gemm_epilogue_plan.restype = i
+    L.gemm_epilogue_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
     L.ta_schedule.restype = i
     L.ta_schedule.argtypes = [i, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
     L.ta_tile_shape.restype = i
@@ -848,12 +852,30 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
+def gemm_epilogue_workspace_bytes(M: int, N: int, num_splits: int) -> int:
+    n = ctypes.c_size_t()
+    rc = lib().gemm_epilogue_workspace_bytes(M, N, num_splits, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
+def gemm_epilogue_plan(M: int, N: int, K: int) -> int:
+    n = ctypes.c_int()
+    rc = lib().gemm_epilogue_plan(M, N, K, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
 def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None, out=None,
-                       out_dtype=None, stream=None):
+                       out_dtype=None, stream=None, num_splits: int | None = None):
     """C = act(A B + bias) + residual for contiguous bfloat16 GPU matrices a [M, K]
     (any M) and b [K, N] (N and K multiples of 8), bias [N] bf16; C and residual
     [M, N] are float32 (default) or bfloat16 (``out_dtype``).  ``activation``:
-    none, relu, gelu (by erf), gelu_tanh or silu.  ``out`` may be ``residual``."""
+    none, relu, gelu (by erf), gelu_tanh or silu.  ``out`` may be ``residual``.  K is
+    summed in ``num_splits`` ranges (default gemm_epilogue_plan), through a workspace
+    allocated here; the default is one range where there is no memory for it."""
     for name, t in (("a", a), ("b", b)):
         if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 2 or not t.is_contiguous():
             raise TypeError(f"{name} must be a contiguous 2-D bfloat16 GPU tensor")
@@ -871,10 +893,21 @@ def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None,
     if residual is not None:
         _vector("residual", residual, dt, (M, N))
     out = _output("out", out, (M, N), dt, a)
+    chosen, ws, need = num_splits is None, None, 0
+    if chosen:
+        num_splits = gemm_epilogue_plan(M, N, K)
+    if num_splits != 1:
+        need = gemm_epilogue_workspace_bytes(M, N, num_splits)
+        try:
+            ws = _workspace(need, a, stream)
+        except torch.OutOfMemoryError:
+            if not chosen:
+                raise
+            num_splits, need = 1, 0   # the caller asked for no workspace: one range needs none
     with _one_device(a, b, bias, residual, out):
         rc = lib().gemm_bf16_epilogue(a.data_ptr(), b.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(),
                                       int(dt == torch.bfloat16), ACTIVATIONS[activation], M, N, K,
-                                      _stream_handle(stream, a))
+                                      num_splits, _ptr(ws), need, _stream_handle(stream, a))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return out

@@ -79,22 +79,41 @@ def test_paged_workspace_and_plan():
 
 
 A, B, BIAS, R, C = (0x100000000 * i for i in range(1, 6))
-GEMM = dict(A=A, B=B, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=136, stream=None)
+GEMM = dict(A=A, B=B, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=136, splits=2, ws=WS,
+            ws_bytes=1 << 20, stream=None)
 
 
 @no_gpu
 @pytest.mark.parametrize("change,status", [
     (dict(A=0), 1), (dict(B=0), 1), (dict(C=0), 1),
     (dict(M=0), 2), (dict(N=0), 2), (dict(K=-8), 2), (dict(N=1 << 24), 2), (dict(K=1 << 22), 2),
-    (dict(M=1 << 20, N=(1 << 20)), 2), (dict(M=1 << 20, K=(1 << 20)), 2),
+    (dict(M=1 << 20, N=1 << 16), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2),
+    (dict(splits=0), 2), (dict(splits=65), 2),
     (dict(N=60), 3), (dict(K=132), 3), (dict(act=-1), 3), (dict(act=5), 3),
     (dict(A=A + 8), 4), (dict(B=B + 2), 4), (dict(C=C + 4), 4), (dict(bias=BIAS + 8), 4), (dict(R=R + 4), 4),
     (dict(C=A + 16), 6), (dict(C=B + 16), 6), (dict(C=BIAS), 6), (dict(R=C + 16), 6), (dict(R=C - 16), 6),
+    (dict(ws=0), 8), (dict(ws_bytes=2 * 40 * 64 * 4 - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=A), 6), (dict(ws=B + 1024), 6),
+    (dict(ws=C - 16), 6), (dict(ws=R), 6), (dict(ws=BIAS), 6),
 ], ids=str)
 def test_gemm_refusals(change, status):
     a = dict(GEMM, **change)
     rc = ta.lib().gemm_bf16_epilogue(*a.values())
     assert rc == status, f"{change}: got {ta.STATUS.get(rc, rc)}, want {ta.STATUS[status]}"
+
+
+def test_gemm_workspace_and_plan():
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 3) == 3 * 40 * 64 * 4
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 1) == 0
+    for M in (1, 16, 40, 65, 300, 4096):
+        for N in (8, 64, 1000, 4096, 65536):
+            for K in (8, 64, 1000, 4096, 65536):
+                assert 1 <= ta.gemm_epilogue_plan(M, N, K) <= 64
+    for bad in [(0, 8, 8), (1, 0, 8), (1, 8, -8), (1, 12, 8), (1, 8, 4), (1, 1 << 24, 8)]:
+        with pytest.raises(ta.TileAttnError):
+            ta.gemm_epilogue_plan(*bad)
+    for bad in [(0, 8, 2), (1, 0, 2), (1, 8, 0), (1, 8, 65)]:
+        with pytest.raises(ta.TileAttnError):
+            ta.gemm_epilogue_workspace_bytes(*bad)
 
 
 torch = pytest.importorskip("torch")

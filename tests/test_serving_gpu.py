@@ -263,13 +263,16 @@ def test_gemm_against_oracle(ta, M, N, K):
         dt = F32 if i % 2 == (M % 2) else BF16
         r = res.to(dt) if has_res else None
         c, tol = serving.gemm_epilogue(f64(a), f64(b), f64(bias) if has_bias else None, act, f64(r) if has_res else None)
-        got = ta.gemm_bf16_epilogue(a, b, bias=bias if has_bias else None, activation=act, residual=r, out_dtype=dt)
-        assert got.dtype == dt and got.shape == (M, N)
-        err = np.abs(f64(got) - c)
         if dt == BF16:
             tol = tol + 2.0 ** -8 * np.abs(c)
-        print(f"  {act} {has_bias} {has_res} {dt}: max error {err.max():.2e}, of bound {(err / tol).max():.2f}", flush=True)
-        assert (err <= tol).all()
+        for splits in (None, 1, 2, 7):
+            got = ta.gemm_bf16_epilogue(a, b, bias=bias if has_bias else None, activation=act, residual=r, out_dtype=dt,
+                                        num_splits=splits)
+            assert got.dtype == dt and got.shape == (M, N)
+            err = np.abs(f64(got) - c)
+            print(f"  {act} {has_bias} {has_res} {dt} splits {splits}: max error {err.max():.2e}, of bound "
+                  f"{(err / tol).max():.2f}", flush=True)
+            assert (err <= tol).all()
 
 
 @pytest.mark.parametrize("M", [1, 40, 300])
@@ -278,9 +281,11 @@ def test_gemm_onto_the_residual_in_place(ta, M, dt):
     g = torch.Generator().manual_seed(M)
     a, b = torch.randn(M, 520, generator=g).to(BF16).cuda(), (torch.randn(520, 264, generator=g) / 20).to(BF16).cuda()
     x = torch.randn(M, 264, generator=g).to(dt).cuda()
-    want = ta.gemm_bf16_epilogue(a, b, residual=x, out_dtype=dt)
-    assert ta.gemm_bf16_epilogue(a, b, residual=x, out=x, out_dtype=dt) is x
-    assert torch.equal(x, want)
+    for splits in (1, 3):
+        y = x.clone()
+        want = ta.gemm_bf16_epilogue(a, b, residual=x, out_dtype=dt, num_splits=splits)
+        assert ta.gemm_bf16_epilogue(a, b, residual=y, out=y, out_dtype=dt, num_splits=splits) is y
+        assert torch.equal(y, want)
 
 
 @pytest.mark.parametrize("M", [1, 20, 100, 300])
