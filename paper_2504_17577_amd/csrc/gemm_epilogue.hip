@@ -4,34 +4,15 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "gemm_tile.h"
 #include "tileattn.h"
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
-}
+using namespace tileattn_gemm;
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-struct EArgs {
-    const uint16_t *A, *B, *bias;
-    const void *R;
-    void *C;
-    float *W;        // with more than one K range: their products [n_split][M][N]
-    int M, N, K;
-    int n_split;
-    int act, c_bf16;
-};
 
 // The two gelus and silu as x times a sigmoid-like factor in (0, 1): no
 // difference of nearly equal numbers for negative x.
@@ -50,27 +31,37 @@ __device__ __forceinline__ f32x4 activated(int act, f32x4 x)
     return x;
 }
 
-// Four columns of a row of C from their fp32 sums (n a multiple of 4, in range)
-__device__ __forceinline__ void store4(const EArgs &a, int m, int n, f32x4 x)
-{
-    const size_t e = (size_t)m * a.N + n;
-    if (a.bias) {
-        const u32x2 b = *(const u32x2 *)(a.bias + n);
-        x += f32x4{bf16_lo(b[0]), bf16_hi(b[0]), bf16_lo(b[1]), bf16_hi(b[1])};
-    }
-    x = activated(a.act, x);
-    if (a.c_bf16) {
-        if (a.R) {
-            const u32x2 r = *(const u32x2 *)((const uint16_t *)a.R + e);
-            x += f32x4{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])};
+// A, B, M, N and K with the tiled kernel's arguments; C is the workspace [n_split]
+// [M][N] there where K is split, `out` the result in any case
+struct EArgs : GArgs {
+    const uint16_t *bias;
+    const void *R;
+    void *out;
+    int act, c_bf16;
+    static constexpr bool EDGE = true;
+
+    // Four columns of a row of the result from their fp32 sums (n a multiple of 4)
+    __device__ __forceinline__ void store(int m, int n, f32x4 x) const
+    {
+        const size_t e = (size_t)m * N + n;
+        if (bias) {
+            const u32x2 b = *(const u32x2 *)(bias + n);
+            x += f32x4{bf16_lo(b[0]), bf16_hi(b[0]), bf16_lo(b[1]), bf16_hi(b[1])};
         }
-        *(u32x2 *)((uint16_t *)a.C + e) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-    } else {
-        if (a.R)
-            x += *(const f32x4 *)((const float *)a.R + e);
-        *(f32x4 *)((float *)a.C + e) = x;
+        x = activated(act, x);
+        if (c_bf16) {
+            if (R) {
+                const u32x2 r = *(const u32x2 *)((const uint16_t *)R + e);
+                x += f32x4{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])};
+            }
+            *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        } else {
+            if (R)
+                x += *(const f32x4 *)((const float *)R + e);
+            *(f32x4 *)((float *)out + e) = x;
+        }
     }
-}
+};
 
 // ---- few rows: up to 64, a decode step's tokens ---------------------------
 // HBM bounds it: every weight is read once and meets a few tokens.  A wave takes
@@ -88,16 +79,16 @@ constexpr int SK_COLS = 128;
 __device__ __forceinline__ uint32_t high16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302); }
 __device__ __forceinline__ uint32_t low16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100); }
 
-template <bool NT>
+template <bool NONTEMP>
 __device__ __forceinline__ u32x4 ld_b(const uint16_t *p)
 {
-    if (NT)
+    if (NONTEMP)
         return __builtin_nontemporal_load((const u32x4 *)p);
     return *(const u32x4 *)p;
 }
 
 // MT: blocks of 16 rows.  SPLIT: to the workspace instead of C
-template <int MT, bool SPLIT, bool NT>
+template <int MT, bool SPLIT, bool NONTEMP>
 __global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
 {
     __shared__ __attribute__((aligned(16))) float red[SK_WAVES][16][SK_COLS];
@@ -136,7 +127,7 @@ __global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
         const int kc = min(k, a.K - 8);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            st.b[i] = ld_b<NT>(bp + (size_t)(kc + i) * a.N);
+            st.b[i] = ld_b<NONTEMP>(bp + (size_t)(kc + i) * a.N);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
             st.x[t] = *(const u32x4 *)(ap + ao[t] + kc);
@@ -203,9 +194,9 @@ __global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
             for (int w = 0; w < SK_WAVES; ++w)
                 sum += *(const f32x4 *)&red[w][x][4 * (ch ^ x)];
             if (SPLIT)
-                *(f32x4 *)(a.W + w0 + (size_t)m * a.N + n) = sum;
+                *(f32x4 *)((float *)a.C + w0 + (size_t)m * a.N + n) = sum;
             else
-                store4(a, m, n, sum);
+                a.store(m, n, sum);
         }
     }
 }
@@ -217,18 +208,19 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(EArgs a)
     const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, mn = (size_t)a.M * a.N;
     if (e >= mn)
         return;
-    f32x4 sum = *(const f32x4 *)(a.W + e);
+    const float *const w = (const float *)a.C;
+    f32x4 sum = *(const f32x4 *)(w + e);
     for (int s = 1; s < a.n_split; s += 8) {
         f32x4 v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u)
-            v[u] = s + u < a.n_split ? *(const f32x4 *)(a.W + (s + u) * mn + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+            v[u] = s + u < a.n_split ? *(const f32x4 *)(w + (s + u) * mn + e) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 8; ++u)
             if (s + u < a.n_split)
                 sum += v[u];
     }
-    store4(a, (int)(e / a.N), (int)(e % a.N), sum);
+    a.store((int)(e / a.N), (int)(e % a.N), sum);
 }
 
 constexpr int MAX_SPLITS = 64;
@@ -243,13 +235,41 @@ hipError_t launch_few(const EArgs &a, bool nt, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t launch(const EArgs &a, hipStream_t s)
+// The tiled kernel (gemm_tile.h), as gemm_bf16 chooses its tiles
+template <int BM, int BN, int ST, int KS>
+hipError_t launch_tiles(EArgs &a, hipStream_t s)
 {
-    const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
-    hipError_t e = a.M <= 16   ? launch_few<1>(a, nt, s)
-                   : a.M <= 32 ? launch_few<2>(a, nt, s)
-                   : a.M <= 48 ? launch_few<3>(a, nt, s)
-                               : launch_few<4>(a, nt, s);
+    constexpr int MF = (BK / 32) % KS == 0 ? 16 : 32;
+    a.tiles_n = (a.N + BN - 1) / BN;
+    a.n_tiles = (a.M + BM - 1) / BM * a.tiles_n;
+    a.n_wg = a.n_tiles * a.n_split;
+    auto kernel = gemm_kernel<BM, BN, ST, KS, MF, false, false, EArgs>;
+    if constexpr (BM == 128)
+        if (a.n_split > 1)
+            kernel = gemm_kernel<BM, BN, ST, KS, MF, false, true, EArgs>;
+    hipLaunchKernelGGL(kernel, dim3(a.n_wg), dim3(NT), 0, s, a);
+    return hipGetLastError();
+}
+
+bool few(int M) { return M <= 64; }
+
+hipError_t launch(EArgs a, hipStream_t s)
+{
+    hipError_t e;
+    if (few(a.M)) {
+        const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
+        e = a.M <= 16   ? launch_few<1>(a, nt, s)
+            : a.M <= 32 ? launch_few<2>(a, nt, s)
+            : a.M <= 48 ? launch_few<3>(a, nt, s)
+                        : launch_few<4>(a, nt, s);
+    } else {
+        const int64_t tiles = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
+        a.n_split = min(a.n_split, (a.K + BK - 1) / BK);
+        e = a.n_split == 1 && (int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256
+                ? launch_tiles<256, 256, 2, 1>(a, s)
+            : tiles * a.n_split <= 256 ? launch_tiles<128, 128, 4, 4>(a, s)
+                                       : launch_tiles<128, 128, 2, 2>(a, s);
+    }
     if (e != hipSuccess || a.n_split == 1)
         return e;
     const size_t threads = (size_t)a.M * a.N / 4;
@@ -312,8 +332,19 @@ ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, con
             overlaps(workspace, w_bytes, residual, c_bytes))
             return TA_ERR_ALIASING;
     }
-    const EArgs a = {(const uint16_t *)A, (const uint16_t *)B, (const uint16_t *)bias, residual, C,
-                     (float *)workspace, M, N, K, num_splits, activation, c_bf16 != 0};
+    EArgs a = {};
+    a.A = (const uint16_t *)A;
+    a.B = (const uint16_t *)B;
+    a.C = workspace;
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    a.n_split = num_splits;
+    a.bias = (const uint16_t *)bias;
+    a.R = residual;
+    a.out = C;
+    a.act = activation;
+    a.c_bf16 = c_bf16 != 0;
     return launch(a, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
 }
 
@@ -334,6 +365,10 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
     const ta_status rc = check_sizes(M, N, K);
     if (rc != TA_OK)
         return rc;
+    if (!few(M)) {
+        *num_splits = 1;
+        return TA_OK;
+    }
     const int strips = (N + SK_COLS - 1) / SK_COLS;
     int sp = 1;
     while (sp < 16 && strips * sp < 256 && K / (sp * 2 * SK_WAVES) >= 32)
