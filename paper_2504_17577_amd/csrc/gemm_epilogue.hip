@@ -15,20 +15,31 @@ __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w 
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // The two gelus and silu as x times a sigmoid-like factor in (0, 1): no
-// difference of nearly equal numbers for negative x.
-__device__ __forceinline__ f32x4 activated(int act, f32x4 x)
+// difference of nearly equal numbers for negative x.  One branch for U quads.
+template <int U>
+__device__ __forceinline__ void activate(int act, f32x4 (&x)[U])
 {
+    auto all = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float v = x[i];
-        x[i] = act == TA_ACT_RELU   ? (v < 0.f ? 0.f : v)
-               : act == TA_ACT_GELU ? 0.5f * v * erfcf(v * -0.70710678118654752440f)
-               : act == TA_ACT_GELU_TANH
-                   ? v / (1.f + expf(-1.59576912160573071176f * (v + 0.044715f * v * v * v)))
-               : act == TA_ACT_SILU ? v / (1.f + expf(-v))
-                                    : v;
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[u][i] = f(x[u][i]);
+    };
+    switch (act) {
+    case TA_ACT_RELU:
+        all([](float v) { return v < 0.f ? 0.f : v; });
+        break;
+    case TA_ACT_GELU:
+        all([](float v) { return 0.5f * v * erfcf(v * -0.70710678118654752440f); });
+        break;
+    case TA_ACT_GELU_TANH:
+        all([](float v) { return v / (1.f + expf(-1.59576912160573071176f * (v + 0.044715f * v * v * v))); });
+        break;
+    case TA_ACT_SILU:
+        all([](float v) { return v / (1.f + expf(-v)); });
+        break;
     }
-    return x;
 }
 
 // A, B, M, N and K with the tiled kernel's arguments; C is the workspace [n_split]
@@ -40,26 +51,52 @@ struct EArgs : GArgs {
     int act, c_bf16;
     static constexpr bool EDGE = true;
 
-    // Four columns of a row of the result from their fp32 sums (n a multiple of 4)
+    // Four columns from n (a multiple of 4) of U rows of the result, from their fp32
+    // sums; what lies past M or N is left out.  The residual's loads come first.
+    template <int U>
+    __device__ __forceinline__ void store(const int (&m)[U], int n, f32x4 (&x)[U]) const
+    {
+        if (n >= N)
+            return;
+        f32x4 r[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            r[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (R && m[u] < M) {
+                const size_t e = (size_t)m[u] * N + n;
+                if (c_bf16) {
+                    const u32x2 w = *(const u32x2 *)((const uint16_t *)R + e);
+                    r[u] = f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
+                } else {
+                    r[u] = *(const f32x4 *)((const float *)R + e);
+                }
+            }
+        }
+        if (bias) {
+            const u32x2 w = *(const u32x2 *)(bias + n);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u] += f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
+        }
+        activate<U>(act, x);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u] += r[u];
+            if (m[u] < M) {
+                const size_t e = (size_t)m[u] * N + n;
+                if (c_bf16)
+                    *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3])};
+                else
+                    *(f32x4 *)((float *)out + e) = x[u];
+            }
+        }
+    }
+
     __device__ __forceinline__ void store(int m, int n, f32x4 x) const
     {
-        const size_t e = (size_t)m * N + n;
-        if (bias) {
-            const u32x2 b = *(const u32x2 *)(bias + n);
-            x += f32x4{bf16_lo(b[0]), bf16_hi(b[0]), bf16_lo(b[1]), bf16_hi(b[1])};
-        }
-        x = activated(act, x);
-        if (c_bf16) {
-            if (R) {
-                const u32x2 r = *(const u32x2 *)((const uint16_t *)R + e);
-                x += f32x4{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])};
-            }
-            *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-        } else {
-            if (R)
-                x += *(const f32x4 *)((const float *)R + e);
-            *(f32x4 *)((float *)out + e) = x;
-        }
+        const int mm[1] = {m};
+        f32x4 xx[1] = {x};
+        store<1>(mm, n, xx);
     }
 };
 

@@ -36,7 +36,8 @@ struct GArgs {
                      // [n_split][M][N], one partial product per range
     int n_wg;        // n_tiles * n_split
     // Whole tiles, C stored as it is.  Arguments with EDGE take any M, and N and K
-    // in multiples of 8, and store by themselves: store(m, n, four columns' sums)
+    // in multiples of 8, and store by themselves: store<U>(m, n, x), four columns
+    // from n (of any n) of U rows (of any m)
     static constexpr bool EDGE = false;
 };
 
@@ -411,32 +412,74 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
             if (g + 1 < KS)
                 __syncthreads();   // read before the next group writes
         }
-        if (kg != 0)
+        if (!EDGE && kg != 0)
             return;
     }
 
     if constexpr (EDGE) {
-        // lane holds row wm + MF i + col, columns wn + MF j + 8 q + 4 half .. + 3
-        // (four such quads of a 32 x 32 block, one of a 16 x 16 block)
-        const size_t w0 = SPLIT ? (size_t)split * a.M * a.N : 0;
+        // Lane holds row wm + MF i + col, columns wn + MF j + 8 q + 4 half .. + 3 (four
+        // such quads of a 32 x 32 block, one of a 16 x 16 block).  The tile goes
+        // through LDS, so that all waves, not one group's two or four, store it (1024 x
+        // 4096 x 4096 with an activation and a residual: 74 us without, see below), row
+        // by row in whole lines, in a loop: the epilogue's code does not fit the
+        // instruction cache if it is unrolled for every accumulator.  A wave's sums
+        // have a part of the four stage buffers (16 or 32 KB, what its pieces of the
+        // groups' sums had); 16-byte chunk c of row r at c ^ (r % chunks of a row).
+        constexpr int ROWB = C::WN * 4, CPR = C::WN / 4;          // bytes and chunks of a part's row
+        constexpr int BUF = KS == 1 ? C::A_BYTES : 16384;         // bytes of a stage buffer
+        constexpr int PART = KS == 1 ? 16384 : C::WM * ROWB;      // bytes of a wave's part
+        constexpr int PH = C::WM * ROWB / PART;                   // row blocks in PH phases
+        constexpr int FP = C::FM / PH, RPP = FP * MF;             // blocks, rows per phase
+        static_assert(C::A_BYTES == C::B_BYTES && C::FM % PH == 0 && BUF % ROWB == 0 &&
+                          PART * (KS == 1 ? 8 : C::WPG) <= 4 * BUF && (KS == 1 || PH == 1), "the waves' parts");
+        auto at = [&](int w, int r, int c) {                      // chunk c of wave w's row r
+            const int o = w * PART + r * ROWB + 16 * (c ^ (r % CPR));
+            unsigned char *const base = o / BUF == 0 ? abuf[0] : o / BUF == 1 ? abuf[1] : o / BUF == 2 ? bbuf[0] : bbuf[1];
+            return (f32x4 *)(base + o % BUF);
+        };
+        // KS = 1: a wave stores its own part; otherwise the eight waves take 16 rows
+        // of all parts each
+        constexpr int CPS = KS == 1 ? CPR : CPR * C::WPG;         // chunks of a row that is stored
+        constexpr int U = 4, RPI = 64 / CPS;                      // steps at a time, rows per step
+        constexpr int RPW = KS == 1 ? RPP : BM / 8;               // rows of a wave
+        static_assert(RPW % (U * RPI) == 0, "whole steps");
+        const int lr = lane / CPS, lc = lane % CPS;
+        const int n = n0 + (KS == 1 ? wn : 0) + 4 * lc, r_first = KS == 1 ? 0 : wave_u * RPW;
+        if (KS == 1)
+            __syncthreads();   // every wave is done with the stage buffers
 #pragma unroll
-        for (int i = 0; i < C::FM; ++i) {
-            const int m = m0 + wm + MF * i + col;
-            if (m < a.M) {
+        for (int ph = 0; ph < PH; ++ph) {
+            if (kg == 0) {
 #pragma unroll
-                for (int j = 0; j < C::FN; ++j)
+                for (int i = 0; i < FP; ++i)
 #pragma unroll
-                    for (int q = 0; q < C::AR / 4; ++q) {
-                        const int n = n0 + wn + MF * j + 8 * q + 4 * half;
-                        const f32x4 x = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
-                                         acc[i][j][4 * q + 3]};
-                        if (n < a.N) {
-                            if (SPLIT)
-                                *(f32x4 *)((float *)a.C + w0 + (size_t)m * a.N + n) = x;
-                            else
-                                a.store(m, n, x);
+                    for (int j = 0; j < C::FN; ++j)
+#pragma unroll
+                        for (int q = 0; q < C::AR / 4; ++q) {
+                            const auto &x = acc[ph * FP + i][j];
+                            *at(KS == 1 ? wave_u : cw, MF * i + col, (MF * j + 8 * q + 4 * half) / 4) =
+                                f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
                         }
-                    }
+            }
+            if (KS > 1)
+                __syncthreads();
+#pragma unroll 1
+            for (int r = r_first + lr; r < r_first + RPW; r += U * RPI) {
+                f32x4 x[U];
+                int m[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    x[u] = *at(KS == 1 ? wave_u : lc / CPR, r + u * RPI, lc % CPR);
+                    m[u] = m0 + (KS == 1 ? wm : 0) + ph * RPP + r + u * RPI;
+                }
+                if (SPLIT) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (m[u] < a.M && n < a.N)
+                            *(f32x4 *)((float *)a.C + ((size_t)split * a.M + m[u]) * a.N + n) = x[u];
+                } else {
+                    a.template store<U>(m, n, x);
+                }
             }
         }
         return;
