@@ -14,6 +14,14 @@ using namespace tileattn_gemm;
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// 1 / (1 + exp(-t)) to 2^-21 + 2^-24 |t|: the hardware's exponential and
+// reciprocal (1 ulp each) instead of the library's (half an ulp, several times the
+// instructions: 10 us of a 4096 x 8192 x 8192 product's 480)
+__device__ __forceinline__ float sigmoid(float t)
+{
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269504088896340736f));
+}
+
 // The two gelus and silu as x times a sigmoid-like factor in (0, 1): no
 // difference of nearly equal numbers for negative x.  One branch for U quads.
 template <int U>
@@ -34,10 +42,10 @@ __device__ __forceinline__ void activate(int act, f32x4 (&x)[U])
         all([](float v) { return 0.5f * v * erfcf(v * -0.70710678118654752440f); });
         break;
     case TA_ACT_GELU_TANH:
-        all([](float v) { return v / (1.f + expf(-1.59576912160573071176f * (v + 0.044715f * v * v * v))); });
+        all([](float v) { return v * sigmoid(1.59576912160573071176f * (v + 0.044715f * v * v * v)); });
         break;
     case TA_ACT_SILU:
-        all([](float v) { return v / (1.f + expf(-v)); });
+        all([](float v) { return v * sigmoid(v); });
         break;
     }
 }
@@ -290,6 +298,26 @@ hipError_t launch_tiles(EArgs &a, hipStream_t s)
 
 bool few(int M) { return M <= 64; }
 
+// Estimates of the tiled kernels' times in us, for the choices below: fitted to
+// products whose B comes from HBM (a model's other weights have passed through
+// the caches since), where a tile of few others to cover its loads costs 0.7 us a
+// step, and two per CU 1.25 together.  kt: steps of 64 rows of B.
+double time_256(int M, int N, int kt)
+{
+    const int64_t tiles = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
+    return (double)((tiles + 255) / 256) * (kt * 1.65 + 15);
+}
+
+double time_128(int M, int N, int kt, int sp)
+{
+    const int64_t wg = (int64_t)((M + 127) / 128) * ((N + 127) / 128) * sp;
+    const int steps = (kt + sp - 1) / sp;
+    const double step = wg <= 256 ? 0.7 : wg <= 512 ? 0.8 + 0.45 * (wg - 256) / 256 : 1.25 * (double)((wg + 511) / 512);
+    const double hbm = (double)kt * 128 * N / 5e6;
+    const double t = 6 + (steps * step > hbm ? steps * step : hbm);
+    return sp == 1 ? t : t + 4 + 8.0 * M * N * sp / 4.5e6;
+}
+
 hipError_t launch(EArgs a, hipStream_t s)
 {
     hipError_t e;
@@ -300,10 +328,10 @@ hipError_t launch(EArgs a, hipStream_t s)
             : a.M <= 48 ? launch_few<3>(a, nt, s)
                         : launch_few<4>(a, nt, s);
     } else {
+        const int kt = (a.K + BK - 1) / BK;
         const int64_t tiles = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
-        a.n_split = min(a.n_split, (a.K + BK - 1) / BK);
-        e = a.n_split == 1 && (int64_t)((a.M + 255) / 256) * ((a.N + 255) / 256) >= 256
-                ? launch_tiles<256, 256, 2, 1>(a, s)
+        a.n_split = min(a.n_split, kt);
+        e = a.n_split == 1 && time_256(a.M, a.N, kt) < time_128(a.M, a.N, kt, 1) ? launch_tiles<256, 256, 2, 1>(a, s)
             : tiles * a.n_split <= 256 ? launch_tiles<128, 128, 4, 4>(a, s)
                                        : launch_tiles<128, 128, 2, 2>(a, s);
     }
@@ -403,7 +431,14 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
     if (rc != TA_OK)
         return rc;
     if (!few(M)) {
+        const int kt = (K + BK - 1) / BK;
+        double best = time_256(M, N, kt);
         *num_splits = 1;
+        for (int sp = 1; sp <= kt && sp <= 32 && (sp == 1 || (int64_t)((M + 127) / 128) * ((N + 127) / 128) * sp <= 512); ++sp)
+            if (time_128(M, N, kt, sp) < best) {
+                best = time_128(M, N, kt, sp);
+                *num_splits = sp;
+            }
         return TA_OK;
     }
     const int strips = (N + SK_COLS - 1) / SK_COLS;

@@ -318,6 +318,7 @@ def test_activations_over_their_range(ta, act):
     want = {"relu": y.clamp(min=0), "gelu": 0.5 * y * torch.erfc(-y / 2 ** 0.5), "silu": y * torch.sigmoid(y),
             "gelu_tanh": y * torch.sigmoid(2 * (2 / np.pi) ** 0.5 * (y + 0.044715 * y ** 3))}[act]
     # 2^-20 of the value, and the argument's own rounding (2^-23 of |x^3| or x^2 at most) in the exponent;
-    # where exp(-u) passes fp32's largest number, 2^128, the result is 0 for x exp(u) < 2^7 2^-128
-    tol = want.abs() * (2.0 ** -20 + 2.0 ** -22 * (1 + y.abs() ** 3).clamp(max=100)) + 2.0 ** -121
+    # where 1 + exp(-u) passes 2^126 its reciprocal is below fp32's smallest normal number, and the
+    # result 0 where it is x exp(u) < 2^7 2^-126
+    tol = want.abs() * (2.0 ** -20 + 2.0 ** -22 * (1 + y.abs() ** 3).clamp(max=100)) + 2.0 ** -119
     assert ((got - want).abs() <= tol).all()
