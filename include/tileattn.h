@@ -524,8 +524,10 @@ typedef enum {
  *   pointers 16-byte aligned; C apart from A, B and bias, and from residual
  *   unless it is C
  *   num_splits  1..64 (else TA_ERR_INVALID_SHAPE): ranges of K that separate
- *               workgroups sum; for more than one, each range's fp32 product
- *               goes to `workspace` (device, 16-byte aligned, at least
+ *               workgroups sum (for more than 64 rows at most K / 64 of them, and
+ *               for the columns only that do not fill the GPU in 256 x 256 tiles);
+ *               for more than one, each range's fp32 product goes to `workspace`
+ *               (device, 16-byte aligned, at least
  *               gemm_epilogue_workspace_bytes(...) bytes, owned by the caller, no
  *               overlap with any other argument; TA_ERR_WORKSPACE if NULL or
  *               smaller) and a second kernel adds them in range order
@@ -538,9 +540,8 @@ ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, con
                              int num_splits, void *workspace, size_t workspace_bytes,
                              void *stream);
 
-/* Workspace bytes gemm_bf16_epilogue needs: num_splits * M * N * 4 for
- * num_splits > 1, 0 for 1.  No HIP call. */
-ta_status gemm_epilogue_workspace_bytes(int M, int N, int num_splits, size_t *bytes);
+/* Workspace bytes gemm_bf16_epilogue needs, 0 for one range.  No HIP call. */
+ta_status gemm_epilogue_workspace_bytes(int M, int N, int K, int num_splits, size_t *bytes);
 
 /* A split count for gemm_bf16_epilogue: 1 unless the workgroups of one range
  * would leave CUs without work.  No HIP call. */

@@ -4,6 +4,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "gemm_tile.h"
 #include "tileattn.h"
 
@@ -51,8 +53,9 @@ __device__ __forceinline__ void activate(int act, f32x4 (&x)[U])
 }
 
 // A, B, M, N and K with the tiled kernel's arguments; C is the workspace [n_split]
-// [M][N] there where K is split, `out` the result in any case
+// [M][N - n_begin] there where K is split, `out` the result in any case
 struct EArgs : GArgs {
+    int n_begin;     // the first column of a launch
     const uint16_t *bias;
     const void *R;
     void *out;
@@ -250,7 +253,8 @@ __global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
 // thread, up to eight ranges' loads in flight.
 __global__ __launch_bounds__(256) void gemm_join_kernel(EArgs a)
 {
-    const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, mn = (size_t)a.M * a.N;
+    const uint32_t width = a.N - a.n_begin;
+    const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, mn = (size_t)a.M * width;
     if (e >= mn)
         return;
     const float *const w = (const float *)a.C;
@@ -265,10 +269,12 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(EArgs a)
             if (s + u < a.n_split)
                 sum += v[u];
     }
-    a.store((int)(e / a.N), (int)(e % a.N), sum);
+    a.store((int)(e / width), a.n_begin + (int)(e % width), sum);
 }
 
 constexpr int MAX_SPLITS = 64;
+
+bool few(int M) { return M <= 64; }
 
 template <int MT>
 hipError_t launch_few(const EArgs &a, bool nt, hipStream_t s)
@@ -280,12 +286,12 @@ hipError_t launch_few(const EArgs &a, bool nt, hipStream_t s)
     return hipGetLastError();
 }
 
-// The tiled kernel (gemm_tile.h), as gemm_bf16 chooses its tiles
+// The tiled kernel (gemm_tile.h) on the columns up to n_end
 template <int BM, int BN, int ST, int KS>
-hipError_t launch_tiles(EArgs &a, hipStream_t s)
+hipError_t launch_tiles(EArgs a, int n_end, hipStream_t s)
 {
     constexpr int MF = (BK / 32) % KS == 0 ? 16 : 32;
-    a.tiles_n = (a.N + BN - 1) / BN;
+    a.tiles_n = (n_end - a.n_begin + BN - 1) / BN;
     a.n_tiles = (a.M + BM - 1) / BM * a.tiles_n;
     a.n_wg = a.n_tiles * a.n_split;
     auto kernel = gemm_kernel<BM, BN, ST, KS, MF, false, false, EArgs>;
@@ -296,17 +302,11 @@ hipError_t launch_tiles(EArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-bool few(int M) { return M <= 64; }
-
 // Estimates of the tiled kernels' times in us, for the choices below: fitted to
 // products whose B comes from HBM (a model's other weights have passed through
 // the caches since), where a tile of few others to cover its loads costs 0.7 us a
 // step, and two per CU 1.25 together.  kt: steps of 64 rows of B.
-double time_256(int M, int N, int kt)
-{
-    const int64_t tiles = (int64_t)((M + 255) / 256) * ((N + 255) / 256);
-    return (double)((tiles + 255) / 256) * (kt * 1.65 + 15);
-}
+double time_256(int kt, int rounds) { return rounds * (kt * 1.65 + 15); }
 
 double time_128(int M, int N, int kt, int sp)
 {
@@ -318,9 +318,48 @@ double time_128(int M, int N, int kt, int sp)
     return sp == 1 ? t : t + 4 + 8.0 * M * N * sp / 4.5e6;
 }
 
+// How a product of more than 64 rows runs: 256 x 256 tiles on its first columns,
+// in whole rounds of one workgroup per CU, and 128 x 128 tiles on the others, with K
+// split in n_split there.  (In 256 x 256 tiles alone 4000 x 8200 x 8200, 528 of
+// them, took three rounds.)
+struct Choice {
+    int n_256;       // columns of the 256 x 256 tiles
+    double time;
+};
+
+Choice choose(int M, int N, int K, int sp)
+{
+    const int kt = (K + BK - 1) / BK, rows = (M + 255) / 256, cols = (N + 255) / 256;
+    const int64_t tiles = (int64_t)rows * cols;
+    Choice best = {0, time_128(M, N, kt, sp)};
+    // the last rounds that are nearly whole, and all tiles
+    const int full = (int)(tiles / 256), all = (int)((tiles + 255) / 256);
+    for (int r = full > 1 ? full - 1 : 1; r <= all; ++r) {
+        const int64_t n1 = (int64_t)r * 256 / rows * 256;
+        if (n1 == 0)
+            continue;
+        const Choice c = n1 >= N ? Choice{N, time_256(kt, r)}
+                                 : Choice{(int)n1, time_256(kt, r) + time_128(M, N - (int)n1, kt, sp)};
+        if (c.time < best.time)
+            best = c;
+    }
+    return best;
+}
+
+// (ranges are whole steps)
+int splits_used(int M, int K, int num_splits) { return few(M) ? num_splits : std::min(num_splits, (K + BK - 1) / BK); }
+
+size_t workspace_need(int M, int N, int K, int num_splits)
+{
+    const int sp = splits_used(M, K, num_splits);
+    const int cols = few(M) ? N : N - choose(M, N, K, sp).n_256;
+    return sp > 1 ? (size_t)sp * M * cols * 4 : 0;
+}
+
 hipError_t launch(EArgs a, hipStream_t s)
 {
-    hipError_t e;
+    hipError_t e = hipSuccess;
+    a.n_split = splits_used(a.M, a.K, a.n_split);
     if (few(a.M)) {
         const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
         e = a.M <= 16   ? launch_few<1>(a, nt, s)
@@ -328,16 +367,22 @@ hipError_t launch(EArgs a, hipStream_t s)
             : a.M <= 48 ? launch_few<3>(a, nt, s)
                         : launch_few<4>(a, nt, s);
     } else {
-        const int kt = (a.K + BK - 1) / BK;
-        const int64_t tiles = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
-        a.n_split = min(a.n_split, kt);
-        e = a.n_split == 1 && time_256(a.M, a.N, kt) < time_128(a.M, a.N, kt, 1) ? launch_tiles<256, 256, 2, 1>(a, s)
-            : tiles * a.n_split <= 256 ? launch_tiles<128, 128, 4, 4>(a, s)
-                                       : launch_tiles<128, 128, 2, 2>(a, s);
+        const Choice c = choose(a.M, a.N, a.K, a.n_split);
+        if (c.n_256) {
+            EArgs first = a;
+            first.n_split = 1;
+            e = launch_tiles<256, 256, 2, 1>(first, c.n_256, s);
+            if (c.n_256 == a.N)
+                return e;
+        }
+        a.n_begin = c.n_256;
+        const int64_t wg = (int64_t)((a.M + 127) / 128) * ((a.N - a.n_begin + 127) / 128) * a.n_split;
+        if (e == hipSuccess)
+            e = wg <= 256 ? launch_tiles<128, 128, 4, 4>(a, a.N, s) : launch_tiles<128, 128, 2, 2>(a, a.N, s);
     }
     if (e != hipSuccess || a.n_split == 1)
         return e;
-    const size_t threads = (size_t)a.M * a.N / 4;
+    const size_t threads = (size_t)a.M * (a.N - a.n_begin) / 4;
     hipLaunchKernelGGL(gemm_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
@@ -386,8 +431,8 @@ ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, con
     if (overlaps(C, c_bytes, A, a_bytes) || overlaps(C, c_bytes, B, b_bytes) ||
         overlaps(C, c_bytes, bias, (size_t)N * 2) || (residual != C && overlaps(C, c_bytes, residual, c_bytes)))
         return TA_ERR_ALIASING;
-    if (num_splits > 1) {
-        const size_t w_bytes = (size_t)num_splits * M * N * 4;
+    const size_t w_bytes = workspace_need(M, N, K, num_splits);
+    if (w_bytes) {
         if (!workspace || workspace_bytes < w_bytes)
             return TA_ERR_WORKSPACE;
         if (misaligned(workspace))
@@ -413,13 +458,16 @@ ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, con
     return launch(a, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
 }
 
-ta_status gemm_epilogue_workspace_bytes(int M, int N, int num_splits, size_t *bytes)
+ta_status gemm_epilogue_workspace_bytes(int M, int N, int K, int num_splits, size_t *bytes)
 {
     if (!bytes)
         return TA_ERR_NULL_POINTER;
-    if (M < 1 || N < 1 || num_splits < 1 || num_splits > MAX_SPLITS)
+    const ta_status rc = check_sizes(M, N, K);
+    if (rc != TA_OK)
+        return rc;
+    if (num_splits < 1 || num_splits > MAX_SPLITS)
         return TA_ERR_INVALID_SHAPE;
-    *bytes = num_splits > 1 ? (size_t)num_splits * M * N * 4 : 0;
+    *bytes = workspace_need(M, N, K, num_splits);
     return TA_OK;
 }
 
@@ -431,12 +479,11 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
     if (rc != TA_OK)
         return rc;
     if (!few(M)) {
-        const int kt = (K + BK - 1) / BK;
-        double best = time_256(M, N, kt);
+        double best = choose(M, N, K, 1).time;
         *num_splits = 1;
-        for (int sp = 1; sp <= kt && sp <= 32 && (sp == 1 || (int64_t)((M + 127) / 128) * ((N + 127) / 128) * sp <= 512); ++sp)
-            if (time_128(M, N, kt, sp) < best) {
-                best = time_128(M, N, kt, sp);
+        for (int sp = 2; sp <= 32 && sp <= (K + BK - 1) / BK; ++sp)
+            if (choose(M, N, K, sp).time < best) {
+                best = choose(M, N, K, sp).time;
                 *num_splits = sp;
             }
         return TA_OK;

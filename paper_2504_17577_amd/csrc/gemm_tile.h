@@ -36,7 +36,7 @@ struct GArgs {
                      // [n_split][M][N], one partial product per range
     int n_wg;        // n_tiles * n_split
     // Whole tiles, C stored as it is.  Arguments with EDGE take any M, and N and K
-    // in multiples of 8, and store by themselves: store<U>(m, n, x), four columns
+    // in multiples of 8, columns from n_begin on, and store by themselves: store<U>(m, n, x), four columns
     // from n (of any n) of U rows (of any m)
     static constexpr bool EDGE = false;
 };
@@ -174,7 +174,10 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
     static_assert(GROUP_M == 4, "the quotient by 1 .. GROUP_M");
     const int tn = rows == 3 ? (int)(((uint64_t)(uint32_t)w * 0xAAAAAAABu) >> 33) : w >> (rows >> 1);
     const int tm = grp * GROUP_M + w - tn * rows;
-    const int m0 = tm * BM, n0 = tn * BN;
+    const int m0 = tm * BM;
+    int n0 = tn * BN;
+    if constexpr (EDGE)
+        n0 += a.n_begin;
     const int cw = KS == 1 ? wave & 3 : wave % C::WPG;    // column of the wave's block
     const int wm = KS == 1 ? (wave >> 2) * C::WM : 0, wn = cw * C::WN;
     const int kg = KS == 1 ? 0 : wave_u / C::WPG;          // this wave's share of each K step
@@ -476,7 +479,8 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
 #pragma unroll
                     for (int u = 0; u < U; ++u)
                         if (m[u] < a.M && n < a.N)
-                            *(f32x4 *)((float *)a.C + ((size_t)split * a.M + m[u]) * a.N + n) = x[u];
+                            *(f32x4 *)((float *)a.C + ((size_t)split * a.M + m[u]) * (a.N - a.n_begin) + n - a.n_begin) =
+                                x[u];
                 } else {
                     a.template store<U>(m, n, x);
                 }

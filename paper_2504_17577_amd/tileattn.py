@@ -116,7 +116,7 @@ def lib():
     L.gemm_bf16_epilogue.restype = i
     L.gemm_bf16_epilogue.argtypes = [p] * 5 + [i] * 6 + [p, ctypes.c_size_t, p]
     L.gemm_epilogue_workspace_bytes.restype = i
-    L.gemm_epilogue_workspace_bytes.argtypes = [i, i, i, ctypes.POINTER(ctypes.c_size_t)]
+    L.gemm_epilogue_workspace_bytes.argtypes = [i, i, i, i, ctypes.POINTER(ctypes.c_size_t)]
     L.gemm_epilogue_plan.restype = i
     L.gemm_epilogue_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
     L.ta_schedule.restype = i
@@ -852,9 +852,9 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
-def gemm_epilogue_workspace_bytes(M: int, N: int, num_splits: int) -> int:
+def gemm_epilogue_workspace_bytes(M: int, N: int, K: int, num_splits: int) -> int:
     n = ctypes.c_size_t()
-    rc = lib().gemm_epilogue_workspace_bytes(M, N, num_splits, ctypes.byref(n))
+    rc = lib().gemm_epilogue_workspace_bytes(M, N, K, num_splits, ctypes.byref(n))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return n.value
@@ -897,9 +897,9 @@ def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None,
     if chosen:
         num_splits = gemm_epilogue_plan(M, N, K)
     if num_splits != 1:
-        need = gemm_epilogue_workspace_bytes(M, N, num_splits)
+        need = gemm_epilogue_workspace_bytes(M, N, K, num_splits)
         try:
-            ws = _workspace(need, a, stream)
+            ws = _workspace(need, a, stream) if need else None
         except torch.OutOfMemoryError:
             if not chosen:
                 raise

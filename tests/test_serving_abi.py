@@ -102,8 +102,12 @@ def test_gemm_refusals(change, status):
 
 
 def test_gemm_workspace_and_plan():
-    assert ta.gemm_epilogue_workspace_bytes(40, 64, 3) == 3 * 40 * 64 * 4
-    assert ta.gemm_epilogue_workspace_bytes(40, 64, 1) == 0
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 512, 3) == 3 * 40 * 64 * 4
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 512, 1) == 0
+    assert ta.gemm_epilogue_workspace_bytes(100, 64, 512, 3) == 3 * 100 * 64 * 4
+    assert ta.gemm_epilogue_workspace_bytes(100, 64, 512, 30) == 8 * 100 * 64 * 4    # eight steps of 64
+    assert ta.gemm_epilogue_workspace_bytes(4096, 8192, 8192, 2) == 0                # whole rounds of large tiles
+    assert ta.gemm_epilogue_workspace_bytes(4000, 8200, 8200, 4) == 4 * 4000 * 8 * 4
     for M in (1, 16, 40, 65, 300, 4096):
         for N in (8, 64, 1000, 4096, 65536):
             for K in (8, 64, 1000, 4096, 65536):
@@ -111,7 +115,7 @@ def test_gemm_workspace_and_plan():
     for bad in [(0, 8, 8), (1, 0, 8), (1, 8, -8), (1, 12, 8), (1, 8, 4), (1, 1 << 24, 8)]:
         with pytest.raises(ta.TileAttnError):
             ta.gemm_epilogue_plan(*bad)
-    for bad in [(0, 8, 2), (1, 0, 2), (1, 8, 0), (1, 8, 65)]:
+    for bad in [(0, 8, 8, 2), (1, 0, 8, 2), (1, 8, 0, 2), (1, 8, 12, 2), (1, 8, 8, 0), (1, 8, 8, 65)]:
         with pytest.raises(ta.TileAttnError):
             ta.gemm_epilogue_workspace_bytes(*bad)
 

@@ -275,6 +275,25 @@ def test_gemm_against_oracle(ta, M, N, K):
             assert (err <= tol).all()
 
 
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 64), (4100, 4104, 72), (4096, 4360, 136), (2000, 16392, 200), (8200, 2050 * 4, 64)])
+def test_gemm_in_large_tiles(ta, M, N, K):
+    """Products with whole rounds of 256 x 256 tiles and other columns after them, the
+    oracle's arithmetic on the GPU (float64)."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    a, b = torch.randn(M, K, generator=g, device="cuda").to(BF16), torch.randn(K, N, generator=g, device="cuda").to(BF16)
+    bias, r = torch.randn(N, generator=g, device="cuda").to(BF16), torch.randn(M, N, generator=g, device="cuda").to(BF16)
+    x = a.double() @ b.double() + bias.double()
+    size = a.double().abs() @ b.double().abs() + bias.double().abs()
+    y = x * torch.sigmoid(x)
+    # as oracle.serving.gemm_epilogue's, and half a step of bf16
+    tol = 1.13 * (K + 2) * 2.0 ** -24 * size + 2.0 ** -20 * y.abs() + (2.0 ** -24 + 2.0 ** -8) * (y + r.double()).abs() + 1e-30
+    for splits in (None, 1, 3):
+        got = ta.gemm_bf16_epilogue(a, b, bias=bias, activation="silu", residual=r, out_dtype=BF16, num_splits=splits)
+        err = (got.double() - y - r.double()).abs()
+        print(f"  splits {splits}: of bound {float((err / tol).max()):.2f}", flush=True)
+        assert (err <= tol).all()
+
+
 @pytest.mark.parametrize("M", [1, 40, 300])
 @pytest.mark.parametrize("dt", [F32, BF16], ids=["fp32", "bf16"])
 def test_gemm_onto_the_residual_in_place(ta, M, dt):
