@@ -62,27 +62,36 @@ struct EArgs : GArgs {
     int act, c_bf16;
     static constexpr bool EDGE = true;
 
-    // Four columns from n (a multiple of 4) of U rows of the result, from their fp32
-    // sums; what lies past M or N is left out.  The residual's loads come first.
+    // The residual of four columns from n (a multiple of 4) of U rows, as it is in
+    // memory (nothing for what lies past M or N)
     template <int U>
-    __device__ __forceinline__ void store(const int (&m)[U], int n, f32x4 (&x)[U]) const
-    {
-        if (n >= N)
-            return;
-        f32x4 r[U];
+    struct Added {
+        u32x4 w[U];
+        __device__ __forceinline__ void load(const EArgs &a, const int (&m)[U], int n)
+        {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            r[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (R && m[u] < M) {
-                const size_t e = (size_t)m[u] * N + n;
-                if (c_bf16) {
-                    const u32x2 w = *(const u32x2 *)((const uint16_t *)R + e);
-                    r[u] = f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
-                } else {
-                    r[u] = *(const f32x4 *)((const float *)R + e);
+            for (int u = 0; u < U; ++u) {
+                w[u] = u32x4{0, 0, 0, 0};
+                if (a.R && m[u] < a.M && n < a.N) {
+                    const size_t e = (size_t)m[u] * a.N + n;
+                    if (a.c_bf16) {
+                        const u32x2 h = *(const u32x2 *)((const uint16_t *)a.R + e);
+                        w[u][0] = h[0];
+                        w[u][1] = h[1];
+                    } else {
+                        w[u] = *(const u32x4 *)((const float *)a.R + e);
+                    }
                 }
             }
         }
+    };
+
+    // These columns and rows of the result from their fp32 sums
+    template <int U>
+    __device__ __forceinline__ void store(const int (&m)[U], int n, f32x4 (&x)[U], const Added<U> &r) const
+    {
+        if (n >= N)
+            return;
         if (bias) {
             const u32x2 w = *(const u32x2 *)(bias + n);
 #pragma unroll
@@ -92,13 +101,17 @@ struct EArgs : GArgs {
         activate<U>(act, x);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            x[u] += r[u];
-            if (m[u] < M) {
-                const size_t e = (size_t)m[u] * N + n;
-                if (c_bf16)
-                    *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3])};
-                else
-                    *(f32x4 *)((float *)out + e) = x[u];
+            if (m[u] >= M)
+                continue;
+            const size_t e = (size_t)m[u] * N + n;
+            if (c_bf16) {
+                if (R)
+                    x[u] += f32x4{bf16_lo(r.w[u][0]), bf16_hi(r.w[u][0]), bf16_lo(r.w[u][1]), bf16_hi(r.w[u][1])};
+                *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3])};
+            } else {
+                if (R)
+                    x[u] += __builtin_bit_cast(f32x4, r.w[u]);
+                *(f32x4 *)((float *)out + e) = x[u];
             }
         }
     }
@@ -107,7 +120,9 @@ struct EArgs : GArgs {
     {
         const int mm[1] = {m};
         f32x4 xx[1] = {x};
-        store<1>(mm, n, xx);
+        Added<1> r;
+        r.load(*this, mm, n);
+        store<1>(mm, n, xx, r);
     }
 };
 

@@ -36,8 +36,8 @@ struct GArgs {
                      // [n_split][M][N], one partial product per range
     int n_wg;        // n_tiles * n_split
     // Whole tiles, C stored as it is.  Arguments with EDGE take any M, and N and K
-    // in multiples of 8, columns from n_begin on, and store by themselves: store<U>(m, n, x), four columns
-    // from n (of any n) of U rows (of any m)
+    // in multiples of 8, columns from n_begin on, and store by themselves, four columns from n (any) of
+    // U rows (any): Added<U>::load(args, m, n), later store(m, n, x, added)
     static constexpr bool EDGE = false;
 };
 
@@ -443,11 +443,24 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
         // KS = 1: a wave stores its own part; otherwise the eight waves take 16 rows
         // of all parts each
         constexpr int CPS = KS == 1 ? CPR : CPR * C::WPG;         // chunks of a row that is stored
-        constexpr int U = 4, RPI = 64 / CPS;                      // steps at a time, rows per step
+        constexpr int U = 8, RPI = 64 / CPS;                      // steps at a time, rows per step
         constexpr int RPW = KS == 1 ? RPP : BM / 8;               // rows of a wave
         static_assert(RPW % (U * RPI) == 0, "whole steps");
         const int lr = lane / CPS, lc = lane % CPS;
         const int n = n0 + (KS == 1 ? wn : 0) + 4 * lc, r_first = KS == 1 ? 0 : wave_u * RPW;
+        auto rows_of = [&](int r, int (&m)[U]) {                  // the rows of C of steps r + u RPI
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                m[u] = m0 + (KS == 1 ? wm : 0) + r + u * RPI;
+        };
+        // What the epilogue adds from memory is loaded eight steps ahead of its use (with
+        // four at a time, each waited for, a round of 256 x 256 tiles stood 30 us)
+        typename Args::template Added<U> now, next;
+        int m[U];
+        if (!SPLIT) {
+            rows_of(r_first + lr, m);
+            now.load(a, m, n);
+        }
         if (KS == 1)
             __syncthreads();   // every wave is done with the stage buffers
 #pragma unroll
@@ -467,22 +480,27 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
             if (KS > 1)
                 __syncthreads();
 #pragma unroll 1
-            for (int r = r_first + lr; r < r_first + RPW; r += U * RPI) {
+            for (int s = 0; s < RPW; s += U * RPI) {
+                const int r = r_first + lr + s;
                 f32x4 x[U];
-                int m[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+                for (int u = 0; u < U; ++u)
                     x[u] = *at(KS == 1 ? wave_u : lc / CPR, r + u * RPI, lc % CPR);
-                    m[u] = m0 + (KS == 1 ? wm : 0) + ph * RPP + r + u * RPI;
-                }
                 if (SPLIT) {
+                    rows_of(r, m);
 #pragma unroll
                     for (int u = 0; u < U; ++u)
                         if (m[u] < a.M && n < a.N)
                             *(f32x4 *)((float *)a.C + ((size_t)split * a.M + m[u]) * (a.N - a.n_begin) + n - a.n_begin) =
                                 x[u];
                 } else {
-                    a.template store<U>(m, n, x);
+                    if (ph * RPP + s + U * RPI < PH * RPW) {
+                        rows_of(ph * RPP + r + U * RPI, m);
+                        next.load(a, m, n);
+                    }
+                    rows_of(ph * RPP + r, m);
+                    a.store(m, n, x, now);
+                    now = next;
                 }
             }
         }
