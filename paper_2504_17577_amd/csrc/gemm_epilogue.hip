@@ -62,18 +62,18 @@ struct EArgs : GArgs {
     int act, c_bf16;
     static constexpr bool EDGE = true;
 
-    // The residual of four columns from n (a multiple of 4) of U rows, as it is in
-    // memory (nothing for what lies past M or N)
+    // The residual of four columns from n (a multiple of 4) of rows m, m + step, ..,
+    // as it is in memory (nothing for what lies past M or N)
     template <int U>
     struct Added {
         u32x4 w[U];
-        __device__ __forceinline__ void load(const EArgs &a, const int (&m)[U], int n)
+        __device__ __forceinline__ void load(const EArgs &a, int m, int step, int n)
         {
+            size_t e = (size_t)m * a.N + n;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u, e += (size_t)step * a.N) {
                 w[u] = u32x4{0, 0, 0, 0};
-                if (a.R && m[u] < a.M && n < a.N) {
-                    const size_t e = (size_t)m[u] * a.N + n;
+                if (a.R && m + u * step < a.M && n < a.N) {
                     if (a.c_bf16) {
                         const u32x2 h = *(const u32x2 *)((const uint16_t *)a.R + e);
                         w[u][0] = h[0];
@@ -88,7 +88,7 @@ struct EArgs : GArgs {
 
     // These columns and rows of the result from their fp32 sums
     template <int U>
-    __device__ __forceinline__ void store(const int (&m)[U], int n, f32x4 (&x)[U], const Added<U> &r) const
+    __device__ __forceinline__ void store(int m, int step, int n, f32x4 (&x)[U], const Added<U> &r) const
     {
         if (n >= N)
             return;
@@ -99,30 +99,34 @@ struct EArgs : GArgs {
                 x[u] += f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
         }
         activate<U>(act, x);
+        size_t e = (size_t)m * N + n;
+        if (c_bf16) {
+            if (R)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (m[u] >= M)
-                continue;
-            const size_t e = (size_t)m[u] * N + n;
-            if (c_bf16) {
-                if (R)
+                for (int u = 0; u < U; ++u)
                     x[u] += f32x4{bf16_lo(r.w[u][0]), bf16_hi(r.w[u][0]), bf16_lo(r.w[u][1]), bf16_hi(r.w[u][1])};
-                *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3])};
-            } else {
-                if (R)
+#pragma unroll
+            for (int u = 0; u < U; ++u, e += (size_t)step * N)
+                if (m + u * step < M)
+                    *(u32x2 *)((uint16_t *)out + e) = u32x2{pack_bf16(x[u][0], x[u][1]), pack_bf16(x[u][2], x[u][3])};
+        } else {
+            if (R)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
                     x[u] += __builtin_bit_cast(f32x4, r.w[u]);
-                *(f32x4 *)((float *)out + e) = x[u];
-            }
+#pragma unroll
+            for (int u = 0; u < U; ++u, e += (size_t)step * N)
+                if (m + u * step < M)
+                    *(f32x4 *)((float *)out + e) = x[u];
         }
     }
 
     __device__ __forceinline__ void store(int m, int n, f32x4 x) const
     {
-        const int mm[1] = {m};
         f32x4 xx[1] = {x};
         Added<1> r;
-        r.load(*this, mm, n);
-        store<1>(mm, n, xx, r);
+        r.load(*this, m, 0, n);
+        store<1>(m, 0, n, xx, r);
     }
 };
 

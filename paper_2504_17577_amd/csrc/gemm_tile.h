@@ -36,8 +36,9 @@ struct GArgs {
                      // [n_split][M][N], one partial product per range
     int n_wg;        // n_tiles * n_split
     // Whole tiles, C stored as it is.  Arguments with EDGE take any M, and N and K
-    // in multiples of 8, columns from n_begin on, and store by themselves, four columns from n (any) of
-    // U rows (any): Added<U>::load(args, m, n), later store(m, n, x, added)
+    // in multiples of 8, columns from n_begin on, and store by themselves, four
+    // columns from n of rows m, m + step .. at a time, of those that there are:
+    // Added<U>::load(args, m, step, n), later store(m, step, n, x, added)
     static constexpr bool EDGE = false;
 };
 
@@ -130,7 +131,8 @@ struct Cfg {
 // of its 64 rows of B is read from the tile's last row or chunk instead, so that
 // nothing outside A and B is addressed; the chunks of a last step that lie past K
 // are then cleared in LDS by the threads whose DMA brought them, in A and in B (a
-// NaN or infinity times zero would not be).  The products are transposed, C^T =
+// NaN or infinity times zero would not be).  That step is by itself: tested for in
+// the loop it cost 4096 x 8192 x 8192 23 us of 420.  The products are transposed, C^T =
 // B^T A^T, which costs nothing (both operands have the same layout) and gives a
 // lane four consecutive columns of a row instead of four rows of a column.
 template <int BM, int BN, int ST, int KS, int MF, bool CBF16, bool SPLIT, class Args = GArgs>
@@ -209,41 +211,17 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
         kt_lo = kt_all * split / a.n_split;
         n_kt = kt_all * (split + 1) / a.n_split - kt_lo;
     }
+    // (the part of a step at K's end comes after the loop, which has no test for it)
+    const int k_part = EDGE && (!SPLIT || split + 1 == (uint32_t)a.n_split) ? a.K % BK : 0;
+    if (k_part)
+        --n_kt;
 
+    const int last_row = EDGE ? min(BM - 1, a.M - 1 - m0) : BM - 1;   // the tile's last row, its columns
+    const int cols = EDGE ? min(BN, a.N - n0) : BN;
     auto dma = [&](int kt, unsigned char *as, unsigned char *bs) {
         const int k0 = (kt_lo + kt) * BK;
-        if constexpr (EDGE) {
-            const int kr = min(a.K - k0, BK);   // rows of B in this step
-            const u32x4s ra = buffer_rsrc(a.A + (size_t)m0 * a.K + k0,
-                                          (uint32_t)(min(BM - 1, a.M - 1 - m0) * a.K + kr) * 2);
-            const u32x4s rb = buffer_rsrc(a.B + (size_t)k0 * a.N + n0,
-                                          (uint32_t)((kr - 1) * a.N + min(BN, a.N - n0)) * 2);
-            const uint32_t la = lds_addr(as), lb = lds_addr(bs);
-            if (kr == BK) {
-#pragma unroll
-                for (int i = 0; i < C::A_PER_THREAD; ++i)
-                    dma16(la + (i * NT + wave_u * 64) * 16, a_off[i], ra);
-#pragma unroll
-                for (int i = 0; i < C::B_PER_THREAD; ++i)
-                    dma16(lb + (i * NT + wave_u * 64) * 16, b_off[i], rb);
-            } else {
-#pragma unroll
-                for (int i = 0; i < C::A_PER_THREAD; ++i) {
-                    const int s = i * NT + wave_u * 64 + lane, r = s / 8, ch = (s % 8) ^ a_swz(r);
-                    dma16(la + (i * NT + wave_u * 64) * 16, a_off[i] - 16 * max(ch - (kr / 8 - 1), 0), ra);
-                }
-#pragma unroll
-                for (int i = 0; i < C::B_PER_THREAD; ++i) {
-                    const int r = (i * NT + wave_u * 64 + lane) / C::BCH;
-                    dma16(lb + (i * NT + wave_u * 64) * 16, b_off[i] - (uint32_t)max(r - (kr - 1), 0) * a.N * 2, rb);
-                }
-            }
-            return;
-        }
-        const u32x4s ra = buffer_rsrc(a.A + (size_t)m0 * a.K + k0,
-                                      (uint32_t)((BM - 1) * a.K + BK) * 2);
-        const u32x4s rb = buffer_rsrc(a.B + (size_t)k0 * a.N + n0,
-                                      (uint32_t)((BK - 1) * a.N + BN) * 2);
+        const u32x4s ra = buffer_rsrc(a.A + (size_t)m0 * a.K + k0, (uint32_t)(last_row * a.K + BK) * 2);
+        const u32x4s rb = buffer_rsrc(a.B + (size_t)k0 * a.N + n0, (uint32_t)((BK - 1) * a.N + cols) * 2);
         const uint32_t la = lds_addr(as), lb = lds_addr(bs);
 #pragma unroll
         for (int i = 0; i < C::A_PER_THREAD; ++i)
@@ -253,11 +231,24 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
             dma16(lb + (i * NT + wave_u * 64) * 16, b_off[i], rb);
     };
 
-    // before the barrier that lets others read step kt: this thread's chunks past K
-    auto clear_past_k = [&](int kt, unsigned char *as, unsigned char *bs) {
-        const int kr = a.K - (kt_lo + kt) * BK;
-        if (!EDGE || kr >= BK)
-            return;
+    // a last step of kr < 64 rows of B
+    auto dma_part = [&](int kr, unsigned char *as, unsigned char *bs) {
+        const int k0 = a.K - kr;
+        const u32x4s ra = buffer_rsrc(a.A + (size_t)m0 * a.K + k0, (uint32_t)(last_row * a.K + kr) * 2);
+        const u32x4s rb = buffer_rsrc(a.B + (size_t)k0 * a.N + n0, (uint32_t)((kr - 1) * a.N + cols) * 2);
+        const uint32_t la = lds_addr(as), lb = lds_addr(bs);
+#pragma unroll
+        for (int i = 0; i < C::A_PER_THREAD; ++i) {
+            const int s = i * NT + wave_u * 64 + lane, ch = (s % 8) ^ a_swz(s / 8);
+            dma16(la + (i * NT + wave_u * 64) * 16, a_off[i] - 16 * max(ch - (kr / 8 - 1), 0), ra);
+        }
+#pragma unroll
+        for (int i = 0; i < C::B_PER_THREAD; ++i) {
+            const int r = (i * NT + wave_u * 64 + lane) / C::BCH;
+            dma16(lb + (i * NT + wave_u * 64) * 16, b_off[i] - (uint32_t)max(r - (kr - 1), 0) * a.N * 2, rb);
+        }
+        // this thread's chunks past K, before the barrier that lets others read
+        wait_dma_all();
 #pragma unroll
         for (int i = 0; i < C::A_PER_THREAD; ++i) {
             const int s = i * NT + wave_u * 64 + lane;
@@ -270,6 +261,7 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
             if (s / C::BCH >= kr)
                 *(u32x4 *)(bs + 16 * s) = u32x4{0, 0, 0, 0};
         }
+        __syncthreads();
     };
 
     Acc acc[C::FM][C::FN];
@@ -326,23 +318,20 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
     };
 
     if constexpr (ST == 2) {
-        dma(0, a0, b0);
+        if (!EDGE || n_kt > 0)
+            dma(0, a0, b0);
         wait_dma_all();
-        clear_past_k(0, a0, b0);
         __syncthreads();
         int kt = 0;
         for (; kt + 1 < n_kt; kt += 2) {
             dma(kt + 1, a1, b1);
             compute(a0, b0);
             wait_dma_all();
-            clear_past_k(kt + 1, a1, b1);
             __syncthreads();
             if (kt + 2 < n_kt)
                 dma(kt + 2, a0, b0);
             compute(a1, b1);
             wait_dma_all();
-            if (EDGE && kt + 2 < n_kt)
-                clear_past_k(kt + 2, a0, b0);
             __syncthreads();
         }
         if (kt < n_kt)
@@ -365,13 +354,18 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
                 wait_dma_upto<C::PER_STAGE>();
             else
                 wait_dma_all();
-            clear_past_k(kt, abuf[kt % ST], bbuf[kt % ST]);
             __syncthreads();
             const int nx = kt + ST - 1;
             if (nx < n_kt)
                 dma(nx, abuf[nx % ST], bbuf[nx % ST]);
             compute(abuf[kt % ST], bbuf[kt % ST]);
         }
+    }
+
+    if (EDGE && k_part) {
+        __syncthreads();   // every wave is done with the stage buffers
+        dma_part(k_part, a0, b0);
+        compute(a0, b0);
     }
 
     if constexpr (KS > 1) {
@@ -443,24 +437,18 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
         // KS = 1: a wave stores its own part; otherwise the eight waves take 16 rows
         // of all parts each
         constexpr int CPS = KS == 1 ? CPR : CPR * C::WPG;         // chunks of a row that is stored
-        constexpr int U = 8, RPI = 64 / CPS;                      // steps at a time, rows per step
+        constexpr int U = KS == 2 ? 4 : 8;                        // steps at a time (128 registers in all)
+        constexpr int RPI = 64 / CPS;                             // rows per step
         constexpr int RPW = KS == 1 ? RPP : BM / 8;               // rows of a wave
         static_assert(RPW % (U * RPI) == 0, "whole steps");
         const int lr = lane / CPS, lc = lane % CPS;
         const int n = n0 + (KS == 1 ? wn : 0) + 4 * lc, r_first = KS == 1 ? 0 : wave_u * RPW;
-        auto rows_of = [&](int r, int (&m)[U]) {                  // the rows of C of steps r + u RPI
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                m[u] = m0 + (KS == 1 ? wm : 0) + r + u * RPI;
-        };
-        // What the epilogue adds from memory is loaded eight steps ahead of its use (with
-        // four at a time, each waited for, a round of 256 x 256 tiles stood 30 us)
+        const int m = m0 + (KS == 1 ? wm : r_first) + lr;          // the row of C of the first step
+        // What the epilogue adds from memory is loaded U steps ahead of its use (with four
+        // at a time, each waited for, a round of 256 x 256 tiles stood 30 us)
         typename Args::template Added<U> now, next;
-        int m[U];
-        if (!SPLIT) {
-            rows_of(r_first + lr, m);
-            now.load(a, m, n);
-        }
+        if (!SPLIT)
+            now.load(a, m, RPI, n);
         if (KS == 1)
             __syncthreads();   // every wave is done with the stage buffers
 #pragma unroll
@@ -486,20 +474,18 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     x[u] = *at(KS == 1 ? wave_u : lc / CPR, r + u * RPI, lc % CPR);
+                const int ms = m + ph * RPP + s;
                 if (SPLIT) {
-                    rows_of(r, m);
+                    const int width = a.N - a.n_begin;
+                    float *to = (float *)a.C + ((size_t)split * a.M + ms) * width + n - a.n_begin;
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (m[u] < a.M && n < a.N)
-                            *(f32x4 *)((float *)a.C + ((size_t)split * a.M + m[u]) * (a.N - a.n_begin) + n - a.n_begin) =
-                                x[u];
+                    for (int u = 0; u < U; ++u, to += RPI * width)
+                        if (ms + u * RPI < a.M && n < a.N)
+                            *(f32x4 *)to = x[u];
                 } else {
-                    if (ph * RPP + s + U * RPI < PH * RPW) {
-                        rows_of(ph * RPP + r + U * RPI, m);
-                        next.load(a, m, n);
-                    }
-                    rows_of(ph * RPP + r, m);
-                    a.store(m, n, x, now);
+                    if (ph * RPP + s + U * RPI < PH * RPW)
+                        next.load(a, ms + U * RPI, RPI, n);
+                    a.store(ms, RPI, n, x, now);
                     now = next;
                 }
             }
