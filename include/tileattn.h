@@ -520,13 +520,14 @@ typedef enum {
  *   C  device, [M, N] row-major: fp32, or bf16 if c_bf16 != 0      written
  *   activation  a ta_activation (else TA_ERR_UNSUPPORTED)
  *   N % 8 == 0 and K % 8 == 0 (else TA_ERR_UNSUPPORTED); N < 2^24, K < 2^22,
- *   M <= 2^20, M * N < 2^36 and M * K < 2^40 (else TA_ERR_INVALID_SHAPE);
+ *   M <= 2^20, M * N < 2^36, M * K < 2^40, N * K < 2^40 (else TA_ERR_INVALID_SHAPE);
  *   pointers 16-byte aligned; C apart from A, B and bias, and from residual
  *   unless it is C
  *   num_splits  1..64 (else TA_ERR_INVALID_SHAPE): ranges of K that separate
- *               workgroups sum (for more than 64 rows at most K / 64 of them, and
- *               for the columns only that do not fill the GPU in 256 x 256 tiles);
- *               for more than one, each range's fp32 product goes to `workspace`
+ *               workgroups sum (up to 64 rows: about this many per 128 columns;
+ *               more rows: at most K / 64 of them, and for the columns only that
+ *               do not fill the GPU in 256 x 256 tiles); for more than one, each
+ *               range's fp32 product goes to `workspace`
  *               (device, 16-byte aligned, at least
  *               gemm_epilogue_workspace_bytes(...) bytes, owned by the caller, no
  *               overlap with any other argument; TA_ERR_WORKSPACE if NULL or

@@ -6,12 +6,15 @@
 
 #include <algorithm>
 
+#include "even_parts.h"
 #include "gemm_tile.h"
 #include "tileattn.h"
 
 namespace {
 
 using namespace tileattn_gemm;
+using tileattn_detail::even_begin;
+using tileattn_detail::even_part_of;
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -138,8 +141,10 @@ struct EArgs : GArgs {
 // v_mfma_f32_16x16x32_bf16, of which operand j is columns 8 c16 + j: nothing of B
 // goes through LDS.  A's operands are 16 bytes of a row as they are, from L2.
 // C^T = B^T A^T, so that a lane ends up with 32 consecutive columns of a token.
-// The waves of a workgroup take ranges of K of their own and add up in LDS, in
-// wave order; with few strips, workgroups take ranges too (n_split).
+// The waves of a workgroup take every eighth step, so that two of them read the
+// halves of A's lines at about the same time, and add up in LDS, in wave order.  A workgroup has a strip to itself or, where strips do not come in
+// whole rounds of one per CU, an even share of all strips' steps (PARTS); strips
+// that a share's ends cut leave partial sums for gemm_few_join_kernel.
 constexpr int SK_WAVES = 8;
 constexpr int SK_COLS = 128;
 
@@ -147,35 +152,44 @@ __device__ __forceinline__ uint32_t high16(uint32_t lo, uint32_t hi) { return __
 __device__ __forceinline__ uint32_t low16(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x05040100); }
 
 template <bool NONTEMP>
-__device__ __forceinline__ u32x4 ld_b(const uint16_t *p)
+__device__ __forceinline__ u32x4 ld_b(const void *p)
 {
     if (NONTEMP)
         return __builtin_nontemporal_load((const u32x4 *)p);
     return *(const u32x4 *)p;
 }
 
-// MT: blocks of 16 rows.  SPLIT: to the workspace instead of C
-template <int MT, bool SPLIT, bool NONTEMP>
-__global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
+// MT: blocks of 16 rows.  parts: 0, or the workgroups that share the steps
+template <int MT, bool NONTEMP>
+__global__ __launch_bounds__(64 * SK_WAVES, MT == 1 ? 4 : 2) void gemm_few_kernel(EArgs a, int parts)
 {
     __shared__ __attribute__((aligned(16))) float red[SK_WAVES][16][SK_COLS];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c16 = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * SK_COLS, m0 = blockIdx.z * (16 * MT);
-    const int rows = min(a.M - m0, 16 * MT);
 
-    // this wave's steps of 32 rows of B
-    const int all = (a.K + 31) / 32, parts = gridDim.y * SK_WAVES, part = blockIdx.y * SK_WAVES + wave;
-    const int s0 = (int)((int64_t)all * part / parts), s1 = (int)((int64_t)all * (part + 1) / parts);
+    // this workgroup's steps of 32 rows of B: from step `at` of a strip, `left` of them
+    const uint32_t all = (a.K + 31) / 32;
+    uint32_t strip = blockIdx.x, at = 0, left = all;
+    if (parts) {
+        const uint32_t n = (a.N + SK_COLS - 1) / SK_COLS * all, begin = even_begin(n, parts, blockIdx.x);
+        left = even_begin(n, parts, blockIdx.x + 1) - begin;
+        strip = begin / all;
+        at = begin % all;
+    }
 
-    // (columns past N read the last eight, rows past M the last: never stored)
-    const uint16_t *const bp = a.B + min(n0 + 8 * c16, a.N - 8);
-    const uint16_t *const ap = a.A + (size_t)m0 * a.K;
+    for (;;) {
+    const uint32_t take = min(left, all - at);
+    const int n0 = strip * SK_COLS;
+    const int s0 = at + wave, s1 = at + take;   // (every eighth step)
+
+    // Bytes of this lane's columns in a row of B, and of its rows of A (columns past N
+    // read the last eight, rows past M the last: never stored)
+    const uint32_t bo = 2 * min(n0 + 8 * c16, a.N - 8);
     uint32_t ao[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
-        ao[t] = (uint32_t)min(16 * t + c16, rows - 1) * a.K;
+        ao[t] = 2 * (uint32_t)min(16 * t + c16, a.M - 1) * a.K;
 
     f32x4 acc[MT][8];
 #pragma unroll
@@ -188,16 +202,17 @@ __global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
         u32x4 b[8], x[MT];
     };
     auto load = [&](int s, Step &st) {
-        const int k = 32 * s + 8 * g;
         // (a last step of fewer rows: the lanes behind them read the last eight,
         // and take zeros below)
-        const int kc = min(k, a.K - 8);
+        const uint32_t k = min(8 * g, a.K - 8 - 32 * s);
+        const unsigned char *bs = (const unsigned char *)(a.B + (size_t)(32 * s) * a.N);
+        const unsigned char *as = (const unsigned char *)(a.A + 32 * s);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            st.b[i] = ld_b<NONTEMP>(bp + (size_t)(kc + i) * a.N);
+            st.b[i] = ld_b<NONTEMP>(bs + (size_t)i * a.N * 2 + (k * 2 * a.N + bo));
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            st.x[t] = *(const u32x4 *)(ap + ao[t] + kc);
+            st.x[t] = *(const u32x4 *)(as + (ao[t] + 2 * k));
     };
     auto compute = [&](int s, Step &st) {
         if (32 * s + 32 > a.K) {
@@ -228,44 +243,82 @@ __global__ __launch_bounds__(64 * SK_WAVES, 2) void gemm_few_kernel(EArgs a)
     Step st[2];
     if (s0 < s1)
         load(s0, st[0]);
-    for (int s = s0; s < s1; s += 2) {
-        if (s + 1 < s1)
-            load(s + 1, st[1]);
+    for (int s = s0; s < s1; s += 2 * SK_WAVES) {
+        if (s + SK_WAVES < s1)
+            load(s + SK_WAVES, st[1]);
         compute(s, st[0]);
-        if (s + 2 < s1)
-            load(s + 2, st[0]);
-        if (s + 1 < s1)
-            compute(s + 1, st[1]);
+        if (s + 2 * SK_WAVES < s1)
+            load(s + 2 * SK_WAVES, st[0]);
+        if (s + SK_WAVES < s1)
+            compute(s + SK_WAVES, st[1]);
     }
 
     // lane: row c16 of the block, columns 32 g + 8 r + j; 16-byte chunk ch of row x
     // at ch ^ x
-    const size_t w0 = SPLIT ? (size_t)blockIdx.y * a.M * a.N : 0;
+    const bool whole = take == all;
+    float *const rec = (float *)a.C + (2 * (size_t)blockIdx.x + (at == 0)) * a.M * SK_COLS;
+    // (the thread's number anew, so that no address below occupies a register while
+    // the steps run)
+    int te = threadIdx.x;
+    asm volatile("" : "+v"(te));
+    const int ce = te & 15, ge = (te & 63) >> 4;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        if (t)
-            __syncthreads();
+        __syncthreads();   // (what was there has been read)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                *(f32x4 *)&red[wave][c16][4 * ((8 * g + 2 * r + q) ^ c16)] =
+                *(f32x4 *)&red[wave][ce][4 * ((8 * ge + 2 * r + q) ^ ce)] =
                     f32x4{acc[t][4 * q][r], acc[t][4 * q + 1][r], acc[t][4 * q + 2][r], acc[t][4 * q + 3][r]};
         __syncthreads();
         static_assert(16 * SK_COLS / 4 == 64 * SK_WAVES, "four columns of a row per thread");
-        const int x = tid / (SK_COLS / 4), ch = tid % (SK_COLS / 4);
-        const int m = m0 + 16 * t + x, n = n0 + 4 * ch;
+        const int x = te / (SK_COLS / 4), ch = te % (SK_COLS / 4);
+        const int m = 16 * t + x, n = n0 + 4 * ch;
         if (m < a.M && n < a.N) {
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < SK_WAVES; ++w)
                 sum += *(const f32x4 *)&red[w][x][4 * (ch ^ x)];
-            if (SPLIT)
-                *(f32x4 *)((float *)a.C + w0 + (size_t)m * a.N + n) = sum;
-            else
+            if (whole)
                 a.store(m, n, sum);
+            else
+                *(f32x4 *)(rec + m * SK_COLS + 4 * ch) = sum;
         }
     }
+    left -= take;
+    if (left == 0)
+        return;
+    ++strip;
+    at = 0;
+    }
+}
+
+// The partial sums of the strips that were cut, added in order of K, and the
+// epilogue: four columns per thread, up to eight records' loads in flight.  Part
+// p's record 2 p is of the strip that an earlier part began, 2 p + 1 of one that it
+// began itself and a later part goes on with.
+__global__ __launch_bounds__(256) void gemm_few_join_kernel(EArgs a, int parts)
+{
+    const uint32_t all = (a.K + 31) / 32, n = (a.N + SK_COLS - 1) / SK_COLS * all, strip = blockIdx.x;
+    const uint32_t p0 = even_part_of(n, parts, strip * all), p1 = even_part_of(n, parts, strip * all + all - 1);
+    const int e = blockIdx.y * 256 + threadIdx.x, m = e / (SK_COLS / 4), col = e % (SK_COLS / 4) * 4;
+    if (p0 == p1 || m >= a.M || (int)(strip * SK_COLS) + col >= a.N)
+        return;
+    const size_t rec = (size_t)a.M * SK_COLS;
+    const float *const w = (const float *)a.C + m * SK_COLS + col;
+    f32x4 sum = *(const f32x4 *)(w + (2 * (size_t)p0 + 1) * rec);
+    for (uint32_t p = p0 + 1; p <= p1; p += 8) {
+        f32x4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = p + u <= p1 ? *(const f32x4 *)(w + 2 * (size_t)(p + u) * rec) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (p + u <= p1)
+                sum += v[u];
+    }
+    a.store(m, strip * SK_COLS + col, sum);
 }
 
 // The ranges' products added in range order, and the epilogue: four columns per
@@ -292,17 +345,37 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(EArgs a)
 }
 
 constexpr int MAX_SPLITS = 64;
+constexpr int FEW_MAX_PARTS = 4096;
 
 bool few(int M) { return M <= 64; }
+
+// The workgroups that share the steps of all strips where num_splits is more than
+// one: about num_splits for each strip, in whole rounds of one per CU, with a step
+// for every wave at least; 0 for a workgroup per strip.
+int few_parts(int N, int K, int num_splits)
+{
+    if (num_splits == 1)
+        return 0;
+    const int64_t strips = (N + SK_COLS - 1) / SK_COLS, most = (strips * ((K + 31) / 32) + SK_WAVES - 1) / SK_WAVES;
+    int64_t parts = strips * num_splits;
+    if (parts > 256)
+        parts -= parts % 256;
+    parts = std::min(std::min(parts, most), (int64_t)FEW_MAX_PARTS);
+    return parts <= strips ? 0 : (int)parts;
+}
 
 template <int MT>
 hipError_t launch_few(const EArgs &a, bool nt, hipStream_t s)
 {
-    const dim3 grid((a.N + SK_COLS - 1) / SK_COLS, a.n_split, (a.M + 16 * MT - 1) / (16 * MT)), block(64 * SK_WAVES);
-    const auto kernel = a.n_split > 1 ? (nt ? gemm_few_kernel<MT, true, true> : gemm_few_kernel<MT, true, false>)
-                                      : (nt ? gemm_few_kernel<MT, false, true> : gemm_few_kernel<MT, false, false>);
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
-    return hipGetLastError();
+    const int strips = (a.N + SK_COLS - 1) / SK_COLS, parts = few_parts(a.N, a.K, a.n_split);
+    const auto kernel = nt ? gemm_few_kernel<MT, true> : gemm_few_kernel<MT, false>;
+    hipLaunchKernelGGL(kernel, dim3(parts ? parts : strips), dim3(64 * SK_WAVES), 0, s, a, parts);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && parts) {
+        hipLaunchKernelGGL(gemm_few_join_kernel, dim3(strips, (a.M * (SK_COLS / 4) + 255) / 256), dim3(256), 0, s, a, parts);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 // The tiled kernel (gemm_tile.h) on the columns up to n_end
@@ -365,40 +438,37 @@ Choice choose(int M, int N, int K, int sp)
     return best;
 }
 
-// (ranges are whole steps)
-int splits_used(int M, int K, int num_splits) { return few(M) ? num_splits : std::min(num_splits, (K + BK - 1) / BK); }
-
 size_t workspace_need(int M, int N, int K, int num_splits)
 {
-    const int sp = splits_used(M, K, num_splits);
-    const int cols = few(M) ? N : N - choose(M, N, K, sp).n_256;
-    return sp > 1 ? (size_t)sp * M * cols * 4 : 0;
+    if (few(M))
+        return (size_t)few_parts(N, K, num_splits) * 2 * M * SK_COLS * 4;
+    const int sp = std::min(num_splits, (K + BK - 1) / BK);   // ranges are whole steps
+    return sp > 1 ? (size_t)sp * M * (N - choose(M, N, K, sp).n_256) * 4 : 0;
 }
 
 hipError_t launch(EArgs a, hipStream_t s)
 {
-    hipError_t e = hipSuccess;
-    a.n_split = splits_used(a.M, a.K, a.n_split);
     if (few(a.M)) {
         const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
-        e = a.M <= 16   ? launch_few<1>(a, nt, s)
-            : a.M <= 32 ? launch_few<2>(a, nt, s)
-            : a.M <= 48 ? launch_few<3>(a, nt, s)
-                        : launch_few<4>(a, nt, s);
-    } else {
-        const Choice c = choose(a.M, a.N, a.K, a.n_split);
-        if (c.n_256) {
-            EArgs first = a;
-            first.n_split = 1;
-            e = launch_tiles<256, 256, 2, 1>(first, c.n_256, s);
-            if (c.n_256 == a.N)
-                return e;
-        }
-        a.n_begin = c.n_256;
-        const int64_t wg = (int64_t)((a.M + 127) / 128) * ((a.N - a.n_begin + 127) / 128) * a.n_split;
-        if (e == hipSuccess)
-            e = wg <= 256 ? launch_tiles<128, 128, 4, 4>(a, a.N, s) : launch_tiles<128, 128, 2, 2>(a, a.N, s);
+        return a.M <= 16   ? launch_few<1>(a, nt, s)
+               : a.M <= 32 ? launch_few<2>(a, nt, s)
+               : a.M <= 48 ? launch_few<3>(a, nt, s)
+                           : launch_few<4>(a, nt, s);
     }
+    hipError_t e = hipSuccess;
+    a.n_split = std::min(a.n_split, (a.K + BK - 1) / BK);
+    const Choice c = choose(a.M, a.N, a.K, a.n_split);
+    if (c.n_256) {
+        EArgs first = a;
+        first.n_split = 1;
+        e = launch_tiles<256, 256, 2, 1>(first, c.n_256, s);
+        if (c.n_256 == a.N)
+            return e;
+    }
+    a.n_begin = c.n_256;
+    const int64_t wg = (int64_t)((a.M + 127) / 128) * ((a.N - a.n_begin + 127) / 128) * a.n_split;
+    if (e == hipSuccess)
+        e = wg <= 256 ? launch_tiles<128, 128, 4, 4>(a, a.N, s) : launch_tiles<128, 128, 2, 2>(a, a.N, s);
     if (e != hipSuccess || a.n_split == 1)
         return e;
     const size_t threads = (size_t)a.M * (a.N - a.n_begin) / 4;
@@ -421,7 +491,8 @@ ta_status check_sizes(int M, int N, int K)
         return TA_ERR_INVALID_SHAPE;
     if (N % 8 || K % 8)
         return TA_ERR_UNSUPPORTED;
-    if (N >= 1 << 24 || K >= 1 << 22 || M > 1 << 20 || (int64_t)M * N >= 1ll << 36 || (int64_t)M * K >= 1ll << 40)
+    if (N >= 1 << 24 || K >= 1 << 22 || M > 1 << 20 || (int64_t)M * N >= 1ll << 36 || (int64_t)M * K >= 1ll << 40 ||
+        (int64_t)N * K >= 1ll << 40)
         return TA_ERR_INVALID_SHAPE;
     return TA_OK;
 }
@@ -507,11 +578,19 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
             }
         return TA_OK;
     }
-    const int strips = (N + SK_COLS - 1) / SK_COLS;
+    // One workgroup per strip where they fill three quarters of their rounds of one
+    // per CU, else several per strip if those do (24 x 14336 x 4096, 112 strips: 38 us
+    // with one, 28 with two, 31 as 256 shares), else even shares of all strips (8 x
+    // 40000 x 4096, 313 strips: 65 us with one each, 57 as 512 shares)
+    const int strips = (N + SK_COLS - 1) / SK_COLS, steps = (K + 31) / 32;
+    const auto fills = [](int wg) { return 4 * (int64_t)wg >= 3 * 256 * (int64_t)((wg + 255) / 256); };
     int sp = 1;
-    while (sp < 16 && strips * sp < 256 && K / (sp * 2 * SK_WAVES) >= 32)
-        sp *= 2;
-    *num_splits = sp;
+    if (!fills(strips)) {
+        sp = std::max(1, 256 / strips);
+        if (!fills(strips * sp))
+            ++sp;
+    }
+    *num_splits = std::max(1, std::min(sp, std::min(steps / SK_WAVES, MAX_SPLITS)));
     return TA_OK;
 }
 

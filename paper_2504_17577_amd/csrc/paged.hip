@@ -258,8 +258,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
         const uint32_t used = paged_parts_used(n, a.parts);
         if (blockIdx.x >= used)
             return;
-        const uint32_t begin = paged_part_begin(n, used, blockIdx.x);
-        left = paged_part_begin(n, used, blockIdx.x + 1) - begin;
+        const uint32_t begin = even_begin(n, used, blockIdx.x);
+        left = even_begin(n, used, blockIdx.x + 1) - begin;
         const Place at = place_of(a, HR, cap, lane, some, begin);
         b = at.b;
         len = at.len;
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
     const uint32_t per = paged_tiles(len, cap);
     const uint32_t t0 = before * HR + hr * per;
     const uint32_t used = paged_parts_used(n, a.parts);
-    const uint32_t p0 = paged_part_of(n, used, t0), p1 = paged_part_of(n, used, t0 + per - 1);
+    const uint32_t p0 = even_part_of(n, used, t0), p1 = even_part_of(n, used, t0 + per - 1);
     if (p0 == p1)
         return;   // a head that one workgroup took whole
     const int h = hr / a.blocks, r0 = (hr % a.blocks) * a.rows;

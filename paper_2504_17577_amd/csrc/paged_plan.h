@@ -3,13 +3,9 @@
 // and host code (its tests too) share it.
 #pragma once
 
-#include <stdint.h>
+#include "even_parts.h"
 
-#ifdef __HIPCC__
-#define PAGED_FN __host__ __device__ inline
-#else
-#define PAGED_FN inline
-#endif
+#define PAGED_FN EVEN_FN
 
 namespace tileattn_detail {
 
@@ -35,19 +31,6 @@ PAGED_FN uint32_t paged_tiles(int len, int cap)
 
 // The first key of tile t of a head
 PAGED_FN int paged_key(uint32_t t) { return t > PAGED_HEAD ? (int)(t - PAGED_HEAD) * PAGED_TILE : 0; }
-
-// n tiles in `parts` parts, as even as they go: the first n % parts get one more
-PAGED_FN uint32_t paged_part_begin(uint32_t n, uint32_t parts, uint32_t p)
-{
-    const uint32_t r = n % parts;
-    return n / parts * p + (p < r ? p : r);
-}
-
-PAGED_FN uint32_t paged_part_of(uint32_t n, uint32_t parts, uint32_t t)
-{
-    const uint32_t q = n / parts, r = n % parts, big = r * (q + 1);
-    return t < big ? t / (q + 1) : r + (t - big) / q;
-}
 
 // The parts that n tiles are cut into where `parts` workgroups run: two tiles each
 // at least (a small batch of long rows in 64-key parts joined 15 % slower)

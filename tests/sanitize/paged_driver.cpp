@@ -28,11 +28,11 @@ static void check_parts(uint32_t n, uint32_t parts)
 {
     const uint32_t used = paged_parts_used(n, parts);
     EXPECT(used >= 1 && used <= parts && used <= n / 2 + n % 2, "used %u", used);
-    EXPECT(paged_part_begin(n, used, 0) == 0 && paged_part_begin(n, used, used) == n, "ends of %u in %u", n, used);
+    EXPECT(even_begin(n, used, 0) == 0 && even_begin(n, used, used) == n, "ends of %u in %u", n, used);
     for (uint32_t p = 0; p < used; ++p) {
-        const uint32_t b = paged_part_begin(n, used, p), e = paged_part_begin(n, used, p + 1);
+        const uint32_t b = even_begin(n, used, p), e = even_begin(n, used, p + 1);
         EXPECT(e > b && e - b <= n / used + 1 && e - b >= n / used, "part %u: %u..%u of %u in %u", p, b, e, n, used);
-        EXPECT(paged_part_of(n, used, b) == p && paged_part_of(n, used, e - 1) == p, "part of %u, %u", b, e - 1);
+        EXPECT(even_part_of(n, used, b) == p && even_part_of(n, used, e - 1) == p, "part of %u, %u", b, e - 1);
     }
 }
 
@@ -47,7 +47,7 @@ static void walk(const int *lens, int B, int cap, uint32_t HR, uint32_t parts)
     const size_t heads = (size_t)B * HR;
     std::vector<int> whole(heads), tiles(heads), record(2 * used, -1);   /* the head of each record */
     for (uint32_t p = 0; p < used; ++p) {
-        uint32_t at = paged_part_begin(n, used, p), left = paged_part_begin(n, used, p + 1) - at, b = 0, first = 0;
+        uint32_t at = even_begin(n, used, p), left = even_begin(n, used, p + 1) - at, b = 0, first = 0;
         while (first + HR * paged_tiles(lens[b], cap) <= at)
             first += HR * paged_tiles(lens[b++], cap);
         uint32_t per = paged_tiles(lens[b], cap), hr = (at - first) / per, t = (at - first) % per;
@@ -75,7 +75,7 @@ static void walk(const int *lens, int B, int cap, uint32_t HR, uint32_t parts)
     for (size_t head = 0; head < heads; ++head) {       /* the merge */
         const uint32_t per = paged_tiles(lens[head / HR], cap);
         EXPECT(tiles[head] == (int)per, "head %zu: %d tiles of %u", head, tiles[head], per);
-        const uint32_t p0 = paged_part_of(n, used, t0), p1 = paged_part_of(n, used, t0 + per - 1);
+        const uint32_t p0 = even_part_of(n, used, t0), p1 = even_part_of(n, used, t0 + per - 1);
         EXPECT(whole[head] == (p0 == p1), "head %zu whole", head);
         if (p0 != p1)
             for (uint32_t p = p0; p <= p1; ++p)

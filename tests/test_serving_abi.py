@@ -79,7 +79,7 @@ def test_paged_workspace_and_plan():
 
 
 A, B, BIAS, R, C = (0x100000000 * i for i in range(1, 6))
-GEMM = dict(A=A, B=B, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=136, splits=2, ws=WS,
+GEMM = dict(A=A, B=B, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=1032, splits=2, ws=WS,
             ws_bytes=1 << 20, stream=None)
 
 
@@ -87,12 +87,12 @@ GEMM = dict(A=A, B=B, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=136, s
 @pytest.mark.parametrize("change,status", [
     (dict(A=0), 1), (dict(B=0), 1), (dict(C=0), 1),
     (dict(M=0), 2), (dict(N=0), 2), (dict(K=-8), 2), (dict(N=1 << 24), 2), (dict(K=1 << 22), 2),
-    (dict(M=1 << 20, N=1 << 16), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2),
+    (dict(M=1 << 20, N=1 << 16), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2), (dict(N=1 << 22, K=1 << 18), 2),
     (dict(splits=0), 2), (dict(splits=65), 2),
     (dict(N=60), 3), (dict(K=132), 3), (dict(act=-1), 3), (dict(act=5), 3),
     (dict(A=A + 8), 4), (dict(B=B + 2), 4), (dict(C=C + 4), 4), (dict(bias=BIAS + 8), 4), (dict(R=R + 4), 4),
     (dict(C=A + 16), 6), (dict(C=B + 16), 6), (dict(C=BIAS), 6), (dict(R=C + 16), 6), (dict(R=C - 16), 6),
-    (dict(ws=0), 8), (dict(ws_bytes=2 * 40 * 64 * 4 - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=A), 6), (dict(ws=B + 1024), 6),
+    (dict(ws=0), 8), (dict(ws_bytes=2 * 2 * 40 * 128 * 4 - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=A), 6), (dict(ws=B + 1024), 6),
     (dict(ws=C - 16), 6), (dict(ws=R), 6), (dict(ws=BIAS), 6),
 ], ids=str)
 def test_gemm_refusals(change, status):
@@ -102,8 +102,13 @@ def test_gemm_refusals(change, status):
 
 
 def test_gemm_workspace_and_plan():
-    assert ta.gemm_epilogue_workspace_bytes(40, 64, 512, 3) == 3 * 40 * 64 * 4
     assert ta.gemm_epilogue_workspace_bytes(40, 64, 512, 1) == 0
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 512, 2) == 2 * 2 * 40 * 128 * 4  # two records of a strip's columns each
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 512, 3) == 2 * 2 * 40 * 128 * 4  # 16 steps for 8 waves: two workgroups
+    assert ta.gemm_epilogue_workspace_bytes(40, 64, 128, 3) == 0                     # four steps: one
+    assert ta.gemm_epilogue_workspace_bytes(8, 14336, 4096, 3) == 256 * 2 * 8 * 128 * 4   # 112 x 3, in whole rounds
+    assert ta.gemm_epilogue_plan(24, 14336, 4096) == 2 and ta.gemm_epilogue_plan(8, 40000, 4096) == 2
+    assert ta.gemm_epilogue_plan(64, 28672, 8192) == 1 and ta.gemm_epilogue_plan(1, 4096, 64) == 1
     assert ta.gemm_epilogue_workspace_bytes(100, 64, 512, 3) == 3 * 100 * 64 * 4
     assert ta.gemm_epilogue_workspace_bytes(100, 64, 512, 30) == 8 * 100 * 64 * 4    # eight steps of 64
     assert ta.gemm_epilogue_workspace_bytes(4096, 8192, 8192, 2) == 0                # whole rounds of large tiles
