@@ -520,7 +520,7 @@ typedef enum {
  *   C  device, [M, N] row-major: fp32, or bf16 if c_bf16 != 0      written
  *   activation  a ta_activation (else TA_ERR_UNSUPPORTED)
  *   N % 8 == 0 and K % 8 == 0 (else TA_ERR_UNSUPPORTED); N < 2^24, K < 2^22,
- *   M <= 2^20, M * N < 2^36, M * K < 2^40, N * K < 2^40 (else TA_ERR_INVALID_SHAPE);
+ *   M <= 2^20, M * N < 2^35, M * K < 2^40, N * K < 2^40 (else TA_ERR_INVALID_SHAPE);
  *   pointers 16-byte aligned; C apart from A, B and bias, and from residual
  *   unless it is C
  *   num_splits  1..64 (else TA_ERR_INVALID_SHAPE): ranges of K that separate

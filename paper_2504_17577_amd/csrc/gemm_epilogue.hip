@@ -491,7 +491,7 @@ ta_status check_sizes(int M, int N, int K)
         return TA_ERR_INVALID_SHAPE;
     if (N % 8 || K % 8)
         return TA_ERR_UNSUPPORTED;
-    if (N >= 1 << 24 || K >= 1 << 22 || M > 1 << 20 || (int64_t)M * N >= 1ll << 36 || (int64_t)M * K >= 1ll << 40 ||
+    if (N >= 1 << 24 || K >= 1 << 22 || M > 1 << 20 || (int64_t)M * N >= 1ll << 35 || (int64_t)M * K >= 1ll << 40 ||
         (int64_t)N * K >= 1ll << 40)
         return TA_ERR_INVALID_SHAPE;
     return TA_OK;

@@ -12,6 +12,7 @@ allocates for itself need no such wait.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -722,38 +723,42 @@ def ssd_forward(x, dt, A, Bm, Cm, D=None, stream=None, num_segments: int | None 
 def _rows(name, t, shape):
     """The element stride between the first-dimension rows of a bf16 GPU tensor of
     this shape whose rows are contiguous (a slice of a wider tensor's columns)."""
-    if t.dtype != torch.bfloat16 or not t.is_cuda or tuple(t.shape) != tuple(shape):
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.shape != shape:
         raise TypeError(f"{name} must be a bfloat16 GPU tensor of shape {tuple(shape)}")
     n, h, d = shape
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+    sn, sh, sd = t.stride()
+    if (d > 1 and sd != 1) or (h > 1 and sh != d):
         raise TypeError(f"{name}: each [{h}, {d}] row must be contiguous")
-    return t.stride(0) if n > 1 else h * d
+    return sn if n > 1 else h * d
+
+
+def _vector(name, t, dtype, shape):
+    # (a torch.Size equals a tuple; built anew for every tensor they cost 2 us a call)
+    if t.dtype != dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
 
 
 def _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table):
     """(Hkv, D, num_pages, page_size, B, max_pages, e4m3) of a paged cache, checked."""
-    e4m3 = k_cache.dtype == torch.float8_e4m3fn
-    if k_cache.dim() != 4 or not (e4m3 or k_cache.dtype == torch.bfloat16):
+    dtype = k_cache.dtype
+    e4m3 = dtype == torch.float8_e4m3fn
+    if k_cache.dim() != 4 or not (e4m3 or dtype == torch.bfloat16):
         raise TypeError("k_cache must be a 4-D bfloat16 or float8_e4m3fn tensor [num_pages, Hkv, page_size, D]")
-    num_pages, Hkv, page_size, D = k_cache.shape
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if t.dtype != k_cache.dtype or not t.is_cuda or tuple(t.shape) != tuple(k_cache.shape) or not t.is_contiguous():
-            raise TypeError(f"{name} must be a contiguous {k_cache.dtype} GPU tensor of shape {tuple(k_cache.shape)}")
-    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-        if t is not None:
-            if not e4m3:
-                raise TileAttnError(3, f"{name} goes with a float8_e4m3fn cache")
-            _vector(name, t, torch.float32, (Hkv,))
+    shape = k_cache.shape
+    num_pages, Hkv, page_size, D = shape
+    _vector("k_cache", k_cache, dtype, shape)
+    _vector("v_cache", v_cache, dtype, shape)
+    if k_scale is not None or v_scale is not None:
+        if not e4m3:
+            raise TileAttnError(3, "k_scale and v_scale go with a float8_e4m3fn cache")
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t is not None:
+                _vector(name, t, torch.float32, (Hkv,))
     if page_table.dim() != 2:
         raise TypeError("page_table must be 2-D [B, max_pages]")
-    B, max_pages = page_table.shape
-    _vector("page_table", page_table, torch.int32, (B, max_pages))
+    B, max_pages = table = page_table.shape
+    _vector("page_table", page_table, torch.int32, table)
     return Hkv, D, num_pages, page_size, B, max_pages, e4m3
-
-
-def _vector(name, t, dtype, shape):
-    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise TypeError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
 
 
 def _ptr(t):
@@ -801,6 +806,12 @@ def attn_paged_plan(B: int, Hq: int, Hkv: int, D: int, page_size: int, max_pages
     return n.value
 
 
+@functools.lru_cache(maxsize=4096)
+def _paged_launch(B, Hq, Hkv, D, page_size, max_pages):
+    n = attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages)
+    return n, attn_paged_workspace_bytes(Hq, Hkv, D, n)
+
+
 def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | None = None,
                       k_scale=None, v_scale=None, num_parts: int | None = None, out=None, lse=None,
                       workspace=None, out_dtype=None, stream=None):
@@ -829,12 +840,14 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
     out = _output("out", out, (B, Hq, D), o_dtype, q)
     lse = _output("lse", lse, (B, Hq), torch.float32, q)
     if num_parts is None:
-        num_parts = attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages)
-    need = attn_paged_workspace_bytes(Hq, Hkv, D, num_parts)
-    if workspace is None and need:
-        workspace = _workspace(need, q, stream)
-    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda
-                                  or not workspace.is_contiguous()):
+        num_parts, need = _paged_launch(B, Hq, Hkv, D, page_size, max_pages)
+    else:
+        need = attn_paged_workspace_bytes(Hq, Hkv, D, num_parts)
+    if workspace is None:
+        if need:
+            workspace = _workspace(need, q, stream)
+    elif (workspace.dtype != torch.uint8 or not workspace.is_cuda
+          or not workspace.is_contiguous()):
         raise TypeError("workspace must be a contiguous uint8 GPU tensor")
     with _one_device(q, k_cache, v_cache, page_table, seq_lens, k_scale, v_scale, out, lse, workspace):
         rc = lib().attn_decode_paged(q.data_ptr(), q_stride, k_cache.data_ptr(), v_cache.data_ptr(),
@@ -868,6 +881,12 @@ def gemm_epilogue_plan(M: int, N: int, K: int) -> int:
     return n.value
 
 
+@functools.lru_cache(maxsize=4096)
+def _epilogue_launch(M, N, K):
+    n = gemm_epilogue_plan(M, N, K)
+    return n, gemm_epilogue_workspace_bytes(M, N, K, n)
+
+
 def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None, out=None,
                        out_dtype=None, stream=None, num_splits: int | None = None):
     """C = act(A B + bias) + residual for contiguous bfloat16 GPU matrices a [M, K]
@@ -883,6 +902,8 @@ def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None,
     K2, N = b.shape
     if K2 != K:
         raise TileAttnError(2, f"inconsistent shapes a{tuple(a.shape)} b{tuple(b.shape)}")
+    if N % 8 or K % 8:
+        raise TileAttnError(3, f"N and K must be multiples of 8 (N={N}, K={K})")
     if activation not in ACTIVATIONS:
         raise TileAttnError(3, f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
     dt = torch.float32 if out_dtype is None else out_dtype
@@ -893,13 +914,14 @@ def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None,
     if residual is not None:
         _vector("residual", residual, dt, (M, N))
     out = _output("out", out, (M, N), dt, a)
-    chosen, ws, need = num_splits is None, None, 0
+    chosen, ws = num_splits is None, None
     if chosen:
-        num_splits = gemm_epilogue_plan(M, N, K)
-    if num_splits != 1:
+        num_splits, need = _epilogue_launch(M, N, K)
+    else:
         need = gemm_epilogue_workspace_bytes(M, N, K, num_splits)
+    if need:
         try:
-            ws = _workspace(need, a, stream) if need else None
+            ws = _workspace(need, a, stream)
         except torch.OutOfMemoryError:
             if not chosen:
                 raise

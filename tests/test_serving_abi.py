@@ -87,7 +87,7 @@ GEMM = dict(A=A, B=B, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=1032, 
 @pytest.mark.parametrize("change,status", [
     (dict(A=0), 1), (dict(B=0), 1), (dict(C=0), 1),
     (dict(M=0), 2), (dict(N=0), 2), (dict(K=-8), 2), (dict(N=1 << 24), 2), (dict(K=1 << 22), 2),
-    (dict(M=1 << 20, N=1 << 16), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2), (dict(N=1 << 22, K=1 << 18), 2),
+    (dict(M=1 << 20, N=1 << 15), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2), (dict(N=1 << 22, K=1 << 18), 2),
     (dict(splits=0), 2), (dict(splits=65), 2),
     (dict(N=60), 3), (dict(K=132), 3), (dict(act=-1), 3), (dict(act=5), 3),
     (dict(A=A + 8), 4), (dict(B=B + 2), 4), (dict(C=C + 4), 4), (dict(bias=BIAS + 8), 4), (dict(R=R + 4), 4),
