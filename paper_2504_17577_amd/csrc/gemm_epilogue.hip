@@ -581,11 +581,13 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
     // One workgroup per strip where they fill three quarters of their rounds of one
     // per CU, else several per strip if those do (24 x 14336 x 4096, 112 strips: 38 us
     // with one, 28 with two, 31 as 256 shares), else even shares of all strips (8 x
-    // 40000 x 4096, 313 strips: 65 us with one each, 57 as 512 shares)
+    // 40000 x 4096, 313 strips: 65 us with one each, 57 as 512 shares).  Up to four
+    // steps a wave the second kernel costs what it saves (8 x 1000 x 1000: 7.0 us
+    // with one, 6.8 with four; x 2048: 10.9 and, with eight, 7.1)
     const int strips = (N + SK_COLS - 1) / SK_COLS, steps = (K + 31) / 32;
     const auto fills = [](int wg) { return 4 * (int64_t)wg >= 3 * 256 * (int64_t)((wg + 255) / 256); };
     int sp = 1;
-    if (!fills(strips)) {
+    if (!fills(strips) && steps > 4 * SK_WAVES) {
         sp = std::max(1, 256 / strips);
         if (!fills(strips * sp))
             ++sp;

@@ -47,7 +47,10 @@ __device__ __forceinline__ float e4m3_arg(float x, float s)
 }
 
 // One thread moves 8 elements (16 bytes) of a token's K or V row: thread i of
-// a token takes chunk i of its 2 Hkv D / 8, K first.
+// a token takes chunk i of its 2 Hkv D / 8, K first.  HBM bounds a prefill (16384
+// tokens of 8 heads of 128 dims, 134 MB read and written: 30.6 us, 4.4 TB/s of the
+// 4.8 that a copy of 4 GiB reaches; with the ordinary cache policy 34), latency a
+// decode step (3 us for 32 tokens).
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
@@ -67,7 +70,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     const int page = a.table[(size_t)sq * a.max_pages + pg];
     if (page < 0 || page >= a.num_pages)
         return;
-    const u32x4 x = *(const u32x4 *)(is_v ? a.V + t * a.v_stride + 8 * c : a.K + t * a.k_stride + 8 * c);
+    const u32x4 x = __builtin_nontemporal_load(
+        (const u32x4 *)(is_v ? a.V + t * a.v_stride + 8 * c : a.K + t * a.k_stride + 8 * c));
     const size_t row = ((((size_t)page * a.Hkv + h) << a.page_shift) + (pos & ((1 << a.page_shift) - 1)));
     void *const to = is_v ? a.Vc : a.Kc;
     if (E4M3) {
@@ -84,7 +88,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
         }
         *(u32x2 *)((uint8_t *)to + row * D + 8 * ch) = y;
     } else {
-        *(u32x4 *)((uint16_t *)to + row * D + 8 * ch) = x;
+        __builtin_nontemporal_store(x, (u32x4 *)((uint16_t *)to + row * D + 8 * ch));
     }
 }
 

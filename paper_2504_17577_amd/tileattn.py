@@ -733,8 +733,9 @@ def _rows(name, t, shape):
 
 
 def _vector(name, t, dtype, shape):
-    # (a torch.Size equals a tuple; built anew for every tensor they cost 2 us a call)
-    if t.dtype != dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
+    # (its device is compared with the others' by _one_device; a torch.Size equals a
+    # tuple, which built anew for every tensor cost 2 us a call)
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
 
 
