@@ -411,9 +411,9 @@ ta_status ssd_segment_heuristic(int batch, int seqlen, int nheads, int *num_segm
  *
  *   K_cache, V_cache  device, [num_pages, Hkv, page_size, D], bf16, or 8-bit
  *                     (OCP e4m3) if cache_e4m3 != 0
- *   k_scale, v_scale  device, fp32 [Hkv], or NULL for 1: an 8-bit number c of
- *                     head h stands for c * scale[h].  NULL for a bf16 cache
- *                     (else TA_ERR_UNSUPPORTED)
+ *   k_scale, v_scale  device, fp32 [Hkv], positive, or NULL for 1: an 8-bit
+ *                     number c of head h stands for c * scale[h].  NULL for a
+ *                     bf16 cache (else TA_ERR_UNSUPPORTED)
  *   page_table        device, int32 [B, max_pages]
  *   D in {64, 128}; page_size a power of two, at least 16 (else
  *   TA_ERR_UNSUPPORTED); max_pages * page_size <= 2^30 and num_pages <= 2^28
@@ -481,7 +481,8 @@ ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_
  *             32 query heads of it), no workspace
  *
  * Entries of page_table past a sequence's last page, and what the caches hold
- * past its last position, are never used.  Scores and sums are fp32; the softmax
+ * past its last position, are never used.  An infinite or NaN key or value of a
+ * sequence makes what it enters infinite or NaN.  Scores and sums are fp32; the softmax
  * weights enter the product with V as two bf16 numbers each (16 bits), three (24
  * bits) for an fp32 O.  Ownership, asynchrony and status codes as attn_fwd.
  */

@@ -1,5 +1,8 @@
 // C = act(A B + bias) + residual for bf16 A [M, K] and B [K, N] on gfx950
-// (MI355X), any M, N and K multiples of 8.
+// (MI355X), any M, N and K multiples of 8.  Up to 64 rows run the kernel below that
+// streams B through registers; more rows the tiled kernel of gemm_tile.h, in 256 x
+// 256 tiles for as many columns as fill whole rounds of one workgroup per CU and in
+// 128 x 128 tiles, with K split if they are few, for the others.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -142,9 +145,13 @@ struct EArgs : GArgs {
 // goes through LDS.  A's operands are 16 bytes of a row as they are, from L2.
 // C^T = B^T A^T, so that a lane ends up with 32 consecutive columns of a token.
 // The waves of a workgroup take every eighth step, so that two of them read the
-// halves of A's lines at about the same time, and add up in LDS, in wave order.  A workgroup has a strip to itself or, where strips do not come in
-// whole rounds of one per CU, an even share of all strips' steps (PARTS); strips
-// that a share's ends cut leave partial sums for gemm_few_join_kernel.
+// halves of A's lines at about the same time, and add up in LDS, in wave order.  A
+// workgroup has a strip to itself or, where strips do not come in whole rounds of
+// one per CU, an even share of all strips' steps (parts); strips that a share's ends
+// cut leave partial sums for gemm_few_join_kernel.
+// Measured, weights from HBM (us, with the join): 1 x 4096 x 4096 12, 24 x 14336 x
+// 4096 28 (4.2 TB/s; the kernel alone 24), 1 x 28672 x 8192 80 (5.9 TB/s), 64 x 28672
+// x 8192 106 (A, which every strip reads from L2, is half of B's bytes there).
 constexpr int SK_WAVES = 8;
 constexpr int SK_COLS = 128;
 
@@ -179,118 +186,117 @@ __global__ __launch_bounds__(64 * SK_WAVES, MT == 1 ? 4 : 2) void gemm_few_kerne
     }
 
     for (;;) {
-    const uint32_t take = min(left, all - at);
-    const int n0 = strip * SK_COLS;
-    const int s0 = at + wave, s1 = at + take;   // (every eighth step)
+        const uint32_t take = min(left, all - at);
+        const int n0 = strip * SK_COLS;
+        const int s0 = at + wave, s1 = at + take;   // (every eighth step)
 
-    // Bytes of this lane's columns in a row of B, and of its rows of A (columns past N
-    // read the last eight, rows past M the last: never stored)
-    const uint32_t bo = 2 * min(n0 + 8 * c16, a.N - 8);
-    uint32_t ao[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-        ao[t] = 2 * (uint32_t)min(16 * t + c16, a.M - 1) * a.K;
-
-    f32x4 acc[MT][8];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    struct Step {
-        u32x4 b[8], x[MT];
-    };
-    auto load = [&](int s, Step &st) {
-        // (a last step of fewer rows: the lanes behind them read the last eight,
-        // and take zeros below)
-        const uint32_t k = min(8 * g, a.K - 8 - 32 * s);
-        const unsigned char *bs = (const unsigned char *)(a.B + (size_t)(32 * s) * a.N);
-        const unsigned char *as = (const unsigned char *)(a.A + 32 * s);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            st.b[i] = ld_b<NONTEMP>(bs + (size_t)i * a.N * 2 + (k * 2 * a.N + bo));
+        // Bytes of this lane's columns in a row of B, and of its rows of A (columns past N
+        // read the last eight, rows past M the last: never stored)
+        const uint32_t bo = 2 * min(n0 + 8 * c16, a.N - 8);
+        uint32_t ao[MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            st.x[t] = *(const u32x4 *)(as + (ao[t] + 2 * k));
-    };
-    auto compute = [&](int s, Step &st) {
-        if (32 * s + 32 > a.K) {
-            const bool in = 32 * s + 8 * g < a.K;
+            ao[t] = 2 * (uint32_t)min(16 * t + c16, a.M - 1) * a.K;
+
+        f32x4 acc[MT][8];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    st.b[i][w] = in ? st.b[i][w] : 0u;
+            for (int j = 0; j < 8; ++j)
+                acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        struct Step {
+            u32x4 b[8], x[MT];
+        };
+        auto load = [&](int s, Step &st) {
+            // (a last step of fewer rows: the lanes behind them read the last eight,
+            // and take zeros below)
+            const uint32_t k = min(8 * g, a.K - 8 - 32 * s);
+            const unsigned char *bs = (const unsigned char *)(a.B + (size_t)(32 * s) * a.N);
+            const unsigned char *as = (const unsigned char *)(a.A + 32 * s);
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    st.x[t][w] = in ? st.x[t][w] : 0u;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            u32x4 v;
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-                v[p] = j & 1 ? high16(st.b[2 * p][j >> 1], st.b[2 * p + 1][j >> 1])
-                             : low16(st.b[2 * p][j >> 1], st.b[2 * p + 1][j >> 1]);
+            for (int i = 0; i < 8; ++i)
+                st.b[i] = ld_b<NONTEMP>(bs + (size_t)i * a.N * 2 + (k * 2 * a.N + bo));
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v),
-                                                                    __builtin_bit_cast(bf16x8, st.x[t]), acc[t][j], 0, 0, 0);
+                st.x[t] = *(const u32x4 *)(as + (ao[t] + 2 * k));
+        };
+        auto compute = [&](int s, Step &st) {
+            if (32 * s + 32 > a.K) {
+                const bool in = 32 * s + 8 * g < a.K;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        st.b[i][w] = in ? st.b[i][w] : 0u;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+                        st.x[t][w] = in ? st.x[t][w] : 0u;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                u32x4 v;
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+                    v[p] = j & 1 ? high16(st.b[2 * p][j >> 1], st.b[2 * p + 1][j >> 1])
+                                 : low16(st.b[2 * p][j >> 1], st.b[2 * p + 1][j >> 1]);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    acc[t][j] = mfma(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, st.x[t]), acc[t][j]);
+            }
+        };
+        Step st[2];
+        if (s0 < s1)
+            load(s0, st[0]);
+        for (int s = s0; s < s1; s += 2 * SK_WAVES) {
+            if (s + SK_WAVES < s1)
+                load(s + SK_WAVES, st[1]);
+            compute(s, st[0]);
+            if (s + 2 * SK_WAVES < s1)
+                load(s + 2 * SK_WAVES, st[0]);
+            if (s + SK_WAVES < s1)
+                compute(s + SK_WAVES, st[1]);
         }
-    };
-    Step st[2];
-    if (s0 < s1)
-        load(s0, st[0]);
-    for (int s = s0; s < s1; s += 2 * SK_WAVES) {
-        if (s + SK_WAVES < s1)
-            load(s + SK_WAVES, st[1]);
-        compute(s, st[0]);
-        if (s + 2 * SK_WAVES < s1)
-            load(s + 2 * SK_WAVES, st[0]);
-        if (s + SK_WAVES < s1)
-            compute(s + SK_WAVES, st[1]);
-    }
 
-    // lane: row c16 of the block, columns 32 g + 8 r + j; 16-byte chunk ch of row x
-    // at ch ^ x
-    const bool whole = take == all;
-    float *const rec = (float *)a.C + (2 * (size_t)blockIdx.x + (at == 0)) * a.M * SK_COLS;
-    // (the thread's number anew, so that no address below occupies a register while
-    // the steps run)
-    int te = threadIdx.x;
-    asm volatile("" : "+v"(te));
-    const int ce = te & 15, ge = (te & 63) >> 4;
+        // lane: row c16 of the block, columns 32 g + 8 r + j; 16-byte chunk ch of row x
+        // at ch ^ x
+        const bool whole = take == all;
+        float *const rec = (float *)a.C + (2 * (size_t)blockIdx.x + (at == 0)) * a.M * SK_COLS;
+        // (the thread's number anew, so that no address below occupies a register while
+        // the steps run)
+        int te = threadIdx.x;
+        asm volatile("" : "+v"(te));
+        const int ce = te & 15, ge = (te & 63) >> 4;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        __syncthreads();   // (what was there has been read)
+        for (int t = 0; t < MT; ++t) {
+            __syncthreads();   // (what was there has been read)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-                *(f32x4 *)&red[wave][ce][4 * ((8 * ge + 2 * r + q) ^ ce)] =
-                    f32x4{acc[t][4 * q][r], acc[t][4 * q + 1][r], acc[t][4 * q + 2][r], acc[t][4 * q + 3][r]};
-        __syncthreads();
-        static_assert(16 * SK_COLS / 4 == 64 * SK_WAVES, "four columns of a row per thread");
-        const int x = te / (SK_COLS / 4), ch = te % (SK_COLS / 4);
-        const int m = 16 * t + x, n = n0 + 4 * ch;
-        if (m < a.M && n < a.N) {
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                for (int q = 0; q < 2; ++q)
+                    *(f32x4 *)&red[wave][ce][4 * ((8 * ge + 2 * r + q) ^ ce)] =
+                        f32x4{acc[t][4 * q][r], acc[t][4 * q + 1][r], acc[t][4 * q + 2][r], acc[t][4 * q + 3][r]};
+            __syncthreads();
+            static_assert(16 * SK_COLS / 4 == 64 * SK_WAVES, "four columns of a row per thread");
+            const int x = te / (SK_COLS / 4), ch = te % (SK_COLS / 4);
+            const int m = 16 * t + x, n = n0 + 4 * ch;
+            if (m < a.M && n < a.N) {
+                f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < SK_WAVES; ++w)
-                sum += *(const f32x4 *)&red[w][x][4 * (ch ^ x)];
-            if (whole)
-                a.store(m, n, sum);
-            else
-                *(f32x4 *)(rec + m * SK_COLS + 4 * ch) = sum;
+                for (int w = 0; w < SK_WAVES; ++w)
+                    sum += *(const f32x4 *)&red[w][x][4 * (ch ^ x)];
+                if (whole)
+                    a.store(m, n, sum);
+                else
+                    *(f32x4 *)(rec + m * SK_COLS + 4 * ch) = sum;
+            }
         }
-    }
-    left -= take;
-    if (left == 0)
-        return;
-    ++strip;
-    at = 0;
+        left -= take;
+        if (left == 0)
+            return;
+        ++strip;
+        at = 0;
     }
 }
 

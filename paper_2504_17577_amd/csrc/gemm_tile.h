@@ -1,6 +1,7 @@
 // The tiled kernel of the bf16 matrix products (gemm.hip, gemm_epilogue.hip):
-// C = A B for A [M, K] and B [K, N], row-major, on the matrix cores.
-// Internal to libtileattn.
+// C = A B for A [M, K] and B [K, N], row-major, on the matrix cores.  Its design is
+// described at the top of gemm.hip, what products of odd sizes and an epilogue add to
+// it at EDGE below.  Internal to libtileattn.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -218,21 +218,30 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 // v_mfma_f32_16x16x32_bf16: S^T = K Q^T, O^T += V^T P^T.
 //
 //  * K and V go from memory to the registers they are used in, nothing through
-//    LDS: a lane's 16 bytes of a K row are its operand of the scores as they are
-//    (8 dims of one key).  Of V a lane loads the same 8 dims of eight keys, the
-//    keys whose weights the scores left in it, and transposes the 8 x 8 block
-//    with byte permutes: operand j of O^T is then dims 8 c16 + j of all lanes.
-//  * A wave takes KS keys a step, on its own, with its own running maximum and
+//    LDS.  A lane's 16 bytes of a K row (8 dims of one key) are its operand of the
+//    scores, after an exchange between two lanes that lets every load take whole
+//    lines.  Of V a lane loads the same 8 dims of eight keys, the keys whose
+//    weights the scores left in it, and transposes the 8 x 8 block with byte
+//    permutes: operand j of O^T is then dims 8 c16 + j of all lanes.
+//  * A wave takes 32 keys a step, on its own, with its own running maximum and
 //    sums; the next K is loaded under the softmax and the product with V, the
-//    next V under the scores.  The NW waves of a workgroup meet in LDS at the end
-//    of a head's keys.
+//    next V under the scores: 16 KB in flight a wave (D = 128, bf16), 128 KB a CU
+//    with two workgroups on it.  The waves of a workgroup take a quarter of its
+//    blocks each and meet in LDS at the end of a head's keys.
 //  * The positions of the whole batch, head by head, are one list of tiles of 16
-//    keys per wave; each workgroup takes an even share of it (parts), so a batch of mixed
-//    lengths occupies the GPU as one of equal ones does, without the host knowing
-//    the lengths.  Heads that a share's ends cut leave partial results for
-//    attn_paged_merge_kernel.
+//    keys per wave; each workgroup takes an even share of it (parts), so a batch
+//    of mixed lengths occupies the GPU as one of equal ones does, without the host
+//    knowing the lengths.  A head counts two tiles more than it has (without, the
+//    shares of many short sequences were the longest: 64 sequences of up to 16384
+//    mixed, 124 us instead of 88).  Heads that a share's ends cut leave partial
+//    results for attn_paged_merge_kernel.
 //  * A 16-key block lies in one page (page_size >= 16), so pages are looked up in
-//    scalar registers, a step ahead.
+//    scalar registers, a step ahead (through the vector loads, behind those of V,
+//    the pages of the next K waited for all of V: 106 us became 139 for B=8 Sk=8191
+//    with one workgroup a head).
+// Measured, kernel without the merge (32 query and 8 K/V heads of 128 dims): B=8
+// Sk=8191 43 us (6.3 TB/s), 64 sequences of up to 16384 mixed, in pages of 16, 75
+// us (6.3 TB/s), B=1 Sk=100001 of 8 bits 35.5 us (5.8 TB/s).
 template <int D, bool E4M3, int RT>
 __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
@@ -611,7 +620,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 // Joins the partial results of the heads that were cut: a workgroup per m_rows
 // query rows of a (sequence, K/V head, row block), several threads per 16 bytes
 // of them that take every n-th record each, U at a time, and meet in LDS.  It is
-// a chain of latencies, so rows get workgroups of their own while there are few.
+// a chain of latencies (4.5 to 6 us), so rows get workgroups of their own while
+// there are few.
 constexpr int MERGE_T = 512;
 template <int D>
 __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, int m_rows)

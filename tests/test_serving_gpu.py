@@ -118,6 +118,7 @@ ATTN = [
     ([513, 2], 40, 2, 64, 128, True),
     ([9001], 8, 2, 128, 64, True),
     (list(range(70)), 2, 2, 64, 16, False),  # more sequences than lanes, most of them short
+    ([7 * i % 90 for i in range(300)], 4, 2, 64, 16, False),
 ]
 
 
