@@ -904,11 +904,15 @@ ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_
     // Two workgroups per CU share the batch, unless the longest sequence the table
     // has room for is short enough for one workgroup a head, which needs no second
     // kernel.  us, one a head | 512 parts (bf16, 128 dims, 32 query and 8 K/V heads):
-    // B=1 500 keys 8.8 | 10.2, 2000 keys 29 | 11; B=64 to 1000 mixed 24 | 18; but
+    // B=1 500 keys 8.8 | 9.8, 2000 keys 29 | 11; B=4 1000 keys 17 | 12.5 (and 4 us less
+    // of the host's time for one launch); B=64 to 1000 mixed 24 | 18; but
     // B=128 (8-bit) to 800 mixed 17 | 23, B=128 16 heads of 64 dims 200 keys 21 | 28.
+    // Where heads are many for the longest sequence's length, its workgroup alone is
+    // not what the call waits for, and no share stops at each of many short heads:
+    // B=128 32 K/V heads of 64 dims to 2000 mixed 64 | 72.
     const int64_t cap = (int64_t)max_pages * page_size;
     const int64_t heads = (int64_t)B * Hkv * paged_row_blocks(Hq / Hkv);
-    *num_parts = cap <= 512 || (cap <= 1024 && heads >= 1024) ? 0 : 512;
+    *num_parts = cap <= 768 || (cap <= 1024 && heads >= 1024) || heads >= 2 * cap ? 0 : 512;
     return TA_OK;
 }
 
