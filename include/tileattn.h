@@ -416,8 +416,8 @@ ta_status ssd_segment_heuristic(int batch, int seqlen, int nheads, int *num_segm
  *                     bf16 cache (else TA_ERR_UNSUPPORTED)
  *   page_table        device, int32 [B, max_pages]
  *   D in {64, 128}; page_size a power of two, at least 16 (else
- *   TA_ERR_UNSUPPORTED); max_pages * page_size <= 2^30 and num_pages <= 2^28
- *   (else TA_ERR_INVALID_SHAPE).  Caches 16-byte aligned, fp32 and int32
+ *   TA_ERR_UNSUPPORTED); max_pages * page_size and Hkv * page_size <= 2^30,
+ *   num_pages <= 2^28, Hkv <= 2^16 (else TA_ERR_INVALID_SHAPE).  Caches 16-byte aligned, fp32 and int32
  *   vectors 4-byte aligned.
  * What the arrays on the device hold cannot be checked before the launch; the
  * kernels check every index they take from them, and address nothing outside
@@ -428,9 +428,10 @@ ta_status ssd_segment_heuristic(int batch, int seqlen, int nheads, int *num_segm
  * kv_cache_append — writes new tokens' keys and values into the paged cache.
  *
  *   K, V      device, bf16 [T, Hkv, D], read only: token t starts k_stride
- *             (v_stride) elements after token t - 1 (at least Hkv * D, a
- *             multiple of 8), so that they can be slices of a fused
- *             projection; 16-byte aligned
+ *             (v_stride) elements after token t - 1 (at least Hkv * D, at most
+ *             2^30, a multiple of 8), so that they can be slices of a fused
+ *             projection; 16-byte aligned.  T >= 1 and T * Hkv * D < 2^34
+ *             (else TA_ERR_INVALID_SHAPE)
  *   seq       device, int32 [T]: token t belongs to sequence seq[t]; NULL:
  *             token t belongs to sequence t (T <= B, else TA_ERR_INVALID_SHAPE)
  *   pos       device, int32 [T]: its position in that sequence.  A token whose
@@ -459,15 +460,17 @@ ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_
  * over its positions t (the new token's own included, once appended).
  *
  *   Q         device, bf16 [B, Hq, D], read only: sequence b starts q_stride
- *             elements after sequence b - 1 (at least Hq * D, a multiple of 8);
- *             16-byte aligned
+ *             elements after sequence b - 1 (at least Hq * D, at most 2^30, a
+ *             multiple of 8); 16-byte aligned
  *   seq_lens  device, int32 [B], from 0 to max_pages * page_size.  Length 0 (an
  *             idle slot of a padded batch) gives O = 0 and LSE = -inf.  Any other
  *             value outside, and a page outside 0..num_pages-1 among those of
  *             the sequence's positions, gives NaN in that sequence's O and LSE
  *   O         device, [B, Hq, D]: fp32, or bf16 if o_bf16 != 0      written
  *   LSE       device, fp32 [B, Hq]                                  written
- *   Hq % Hkv == 0, Hq <= 65536, B * Hq < 2^24 (else TA_ERR_INVALID_SHAPE);
+ *   Hq % Hkv == 0, Hq <= 65536, B * Hq < 2^24, and less than 2^31 for B * Hkv *
+ *   ceil(Hq / Hkv / 32) * (max_pages * page_size / 64 + 3), the units of 64
+ *   positions that the batch could come to (else TA_ERR_INVALID_SHAPE);
  *   scale >= 0, finite; O and LSE 16-byte aligned and apart from each other and
  *   from every input (TA_ERR_ALIASING)
  *   num_parts 0..4096 (else TA_ERR_INVALID_SHAPE): the cached positions of the

@@ -595,7 +595,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                     rec[((size_t)(a.rows + 3) & ~3) * (D + 1) + x] = l;
                 }
             } else {
-                o *= bad_len ? NAN : l == 0.f ? 0.f : vs / l;
+                o *= bad_len ? NAN : len == 0 ? 0.f : vs / l;   // (every score -inf: 0 / 0)
                 const size_t at = (row0 + x) * D + 4 * ch;
                 if (a.o_bf16)
                     *(u32x2 *)((uint16_t *)a.O + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
                 l = l * f0 + sl[s] * f1;
                 o = o * f0 + *(const f32x4 *)so[s] * f1;
             }
-            o *= bad_len ? NAN : l == 0.f ? 0.f : vs / l;
+            o *= bad_len ? NAN : len == 0 ? 0.f : vs / l;
             const size_t at = (row0 + x) * D + 4 * ch;
             if (a.o_bf16)
                 *(u32x2 *)((uint16_t *)a.O + at) = u32x2{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])};

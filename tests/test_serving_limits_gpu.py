@@ -126,6 +126,25 @@ def test_one_scale_without_the_other(ta, which):
             assert torch.equal(c[table[b, t // 16].long(), :, t % 16].view(torch.uint8), want.view(torch.uint8))
 
 
+@pytest.mark.parametrize("parts", [0, 7])
+@pytest.mark.parametrize("n", [1, 16, 300])
+def test_every_score_minus_infinity(ta, n, parts):
+    """The weights are 0 / 0: NaN, not the zeros of an idle slot."""
+    D, P = 64, 16
+    per = -(-n // P)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    kc, vc = (torch.randn(2 * per, 1, P, D, generator=g, device="cuda").to(BF16) for _ in range(2))
+    table = torch.arange(2 * per, dtype=I32, device="cuda").view(2, per)
+    lens = torch.tensor([n, 0], dtype=I32, device="cuda")
+    kc[:, :, :, 5] = float("-inf")
+    q = torch.rand(2, 3, D, generator=g, device="cuda").add(0.5).to(BF16)
+    o, lse = ta.attn_decode_paged(q, kc, vc, table, lens, num_parts=parts)
+    assert torch.isnan(o[0]).all() and torch.isneginf(lse[0]).all()
+    assert (o[1] == 0).all() and torch.isneginf(lse[1]).all()
+    want = plain(q[:1], kc, vc, table, lens[:1], 0.125)
+    assert torch.isnan(want[0]).all() and torch.isneginf(want[1]).all()
+
+
 def test_two_tokens_for_one_place(ta):
     """Which of them it holds is not defined; that it holds one of them, piece by piece,
     and that nothing else is touched, is."""
