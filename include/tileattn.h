@@ -485,9 +485,10 @@ ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_
  *
  * Entries of page_table past a sequence's last page, and what the caches hold
  * past its last position, are never used.  An infinite or NaN key or value of a
- * sequence makes what it enters infinite or NaN.  Scores and sums are fp32; the softmax
- * weights enter the product with V as two bf16 numbers each (16 bits), three (24
- * bits) for an fp32 O.  Ownership, asynchrony and status codes as attn_fwd.
+ * sequence makes what it enters infinite or NaN.  Scores, softmax weights and sums
+ * are fp32; the weights enter the product with V with all 24 bits, as three bf16
+ * numbers each.  A bf16 O is the fp32 one, rounded once, to nearest even.
+ * Ownership, asynchrony and status codes as attn_fwd.
  */
 ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache,
                             const void *V_cache, int cache_e4m3, const float *k_scale,

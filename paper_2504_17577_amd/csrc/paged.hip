@@ -494,9 +494,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             }
 #pragma unroll
             for (int kp = 0; kp < KB / 2; ++kp) {
-                // The weights as bf16 numbers that add up to 16 of their 24 bits, or
-                // all of them: what is cut off here would be the largest error of O,
-                // and the matrix cores have the time
+                // The weights as three bf16 numbers that add up to all their 24 bits: with
+                // two, cut off, a bf16 O was not the nearest number to the exact one in 215
+                // of 32768 places (B=8 Sk=8191; 25 with an fp32 softmax by itself).  The
+                // loads leave the matrix cores the time: 49 us with two and with three, 8
+                // sequences of 8000 with 32 query heads to a K/V head 26.8 and 27.4
                 bf16x8 p[RT][3];
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
@@ -532,17 +534,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                     const bf16x8 v0 = __builtin_bit_cast(bf16x8, u32x4{x0[0], x0[1], x0[2], x0[3]});
                     const bf16x8 v1 = __builtin_bit_cast(bf16x8, u32x4{x1[0], x1[1], x1[2], x1[3]});
 #pragma unroll
-                    for (int i = 0; i < RT; ++i) {
+                    for (int i = 0; i < RT; ++i)
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
+                        for (int n = 0; n < 3; ++n) {
                             acc[i][j] = mfma(v0, p[i][n], acc[i][j]);
                             acc[i][j + 1] = mfma(v1, p[i][n], acc[i][j + 1]);
                         }
-                        if (!a.o_bf16) {
-                            acc[i][j] = mfma(v0, p[i][2], acc[i][j]);
-                            acc[i][j + 1] = mfma(v1, p[i][2], acc[i][j + 1]);
-                        }
-                    }
                 }
             }
             if (s + 1 < steps)
