@@ -22,17 +22,32 @@ using tileattn_detail::even_part_of;
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// 1 / (1 + exp(-t)) to 2^-21 + 2^-24 |t|: the hardware's exponential and
-// reciprocal (1 ulp each) instead of the library's (half an ulp, several times the
-// instructions: 10 us of a 4096 x 8192 x 8192 product's 480)
+// 1 / (1 + exp(-t)) by the hardware's exponential and reciprocal (1 ulp each) instead
+// of the library's (half an ulp, several times the instructions: 10 us of a 4096 x
+// 8192 x 8192 product's 480).  The exponent u = -t log2(e) is rounded, and so the value
+// off by up to 2^-21 + 1.25 2^-24 |t| of itself (4e-6 at -87; below that the reciprocal
+// is less than the smallest normal number, and 0).  A bf16 result, rounded by 2^-8,
+// takes it so.
+// FINE, for an fp32 result: within 2^-21 + 2^-22 |t| / 87 of the value down to 2^-128,
+// then 0.  What the rounding left out of the exponent, d = -t - u ln 2 (ln 2 as one fp32
+// number is the second term), goes into the exponential as 1 + d, and the reciprocal is
+// taken of a fourth of the sum.  4096 x 8192 x 1024, silu, fp32 C: 82.4 us without, 84.0
+// with; in the kernels of a bf16 C, 75 without and 80 with.
+template <bool FINE>
 __device__ __forceinline__ float sigmoid(float t)
 {
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269504088896340736f));
+    const float u = t * -1.44269504088896340736f;
+    float e = __builtin_amdgcn_exp2f(u);
+    if (!FINE)
+        return __builtin_amdgcn_rcpf(1.f + e);
+    const float d = __builtin_fmaf(u, -0.69314718055994530942f, -t);
+    e = fabsf(u) < 128.f ? __builtin_fmaf(e, d, e) : e;   // (0 and infinity as they are)
+    return 0.25f * __builtin_amdgcn_rcpf(__builtin_fmaf(e, 0.25f, 0.25f));
 }
 
 // The two gelus and silu as x times a sigmoid-like factor in (0, 1): no
 // difference of nearly equal numbers for negative x.  One branch for U quads.
-template <int U>
+template <bool FINE, int U>
 __device__ __forceinline__ void activate(int act, f32x4 (&x)[U])
 {
     auto all = [&](auto f) {
@@ -50,22 +65,23 @@ __device__ __forceinline__ void activate(int act, f32x4 (&x)[U])
         all([](float v) { return 0.5f * v * erfcf(v * -0.70710678118654752440f); });
         break;
     case TA_ACT_GELU_TANH:
-        all([](float v) { return v * sigmoid(1.59576912160573071176f * (v + 0.044715f * v * v * v)); });
+        all([](float v) { return v * sigmoid<FINE>(1.59576912160573071176f * (v + 0.044715f * v * v * v)); });
         break;
     case TA_ACT_SILU:
-        all([](float v) { return v * sigmoid(v); });
+        all([](float v) { return v * sigmoid<FINE>(v); });
         break;
     }
 }
 
 // A, B, M, N and K with the tiled kernel's arguments; C is the workspace [n_split]
 // [M][N - n_begin] there where K is split, `out` the result in any case
+template <bool CBF16>
 struct EArgs : GArgs {
     int n_begin;     // the first column of a launch
     const uint16_t *bias;
     const void *R;
     void *out;
-    int act, c_bf16;
+    int act;
     static constexpr bool EDGE = true;
 
     // The residual of four columns from n (a multiple of 4) of rows m, m + step, ..,
@@ -80,7 +96,7 @@ struct EArgs : GArgs {
             for (int u = 0; u < U; ++u, e += (size_t)step * a.N) {
                 w[u] = u32x4{0, 0, 0, 0};
                 if (a.R && m + u * step < a.M && n < a.N) {
-                    if (a.c_bf16) {
+                    if constexpr (CBF16) {
                         const u32x2 h = *(const u32x2 *)((const uint16_t *)a.R + e);
                         w[u][0] = h[0];
                         w[u][1] = h[1];
@@ -104,9 +120,9 @@ struct EArgs : GArgs {
             for (int u = 0; u < U; ++u)
                 x[u] += f32x4{bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1])};
         }
-        activate<U>(act, x);
+        activate<!CBF16>(act, x);
         size_t e = (size_t)m * N + n;
-        if (c_bf16) {
+        if constexpr (CBF16) {
             if (R)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -167,8 +183,8 @@ __device__ __forceinline__ u32x4 ld_b(const void *p)
 }
 
 // MT: blocks of 16 rows.  parts: 0, or the workgroups that share the steps
-template <int MT, bool NONTEMP>
-__global__ __launch_bounds__(64 * SK_WAVES, MT == 1 ? 4 : 2) void gemm_few_kernel(EArgs a, int parts)
+template <bool CBF16, int MT, bool NONTEMP>
+__global__ __launch_bounds__(64 * SK_WAVES, MT == 1 ? 4 : 2) void gemm_few_kernel(EArgs<CBF16> a, int parts)
 {
     __shared__ __attribute__((aligned(16))) float red[SK_WAVES][16][SK_COLS];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -304,7 +320,8 @@ __global__ __launch_bounds__(64 * SK_WAVES, MT == 1 ? 4 : 2) void gemm_few_kerne
 // epilogue: four columns per thread, up to eight records' loads in flight.  Part
 // p's record 2 p is of the strip that an earlier part began, 2 p + 1 of one that it
 // began itself and a later part goes on with.
-__global__ __launch_bounds__(256) void gemm_few_join_kernel(EArgs a, int parts)
+template <bool CBF16>
+__global__ __launch_bounds__(256) void gemm_few_join_kernel(EArgs<CBF16> a, int parts)
 {
     const uint32_t all = (a.K + 31) / 32, n = (a.N + SK_COLS - 1) / SK_COLS * all, strip = blockIdx.x;
     const uint32_t p0 = even_part_of(n, parts, strip * all), p1 = even_part_of(n, parts, strip * all + all - 1);
@@ -329,7 +346,8 @@ __global__ __launch_bounds__(256) void gemm_few_join_kernel(EArgs a, int parts)
 
 // The ranges' products added in range order, and the epilogue: four columns per
 // thread, up to eight ranges' loads in flight.
-__global__ __launch_bounds__(256) void gemm_join_kernel(EArgs a)
+template <bool CBF16>
+__global__ __launch_bounds__(256) void gemm_join_kernel(EArgs<CBF16> a)
 {
     const uint32_t width = a.N - a.n_begin;
     const size_t e = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4, mn = (size_t)a.M * width;
@@ -370,32 +388,32 @@ int few_parts(int N, int K, int num_splits)
     return parts <= strips ? 0 : (int)parts;
 }
 
-template <int MT>
-hipError_t launch_few(const EArgs &a, bool nt, hipStream_t s)
+template <int MT, bool CBF16>
+hipError_t launch_few(const EArgs<CBF16> &a, bool nt, hipStream_t s)
 {
     const int strips = (a.N + SK_COLS - 1) / SK_COLS, parts = few_parts(a.N, a.K, a.n_split);
-    const auto kernel = nt ? gemm_few_kernel<MT, true> : gemm_few_kernel<MT, false>;
+    const auto kernel = nt ? gemm_few_kernel<CBF16, MT, true> : gemm_few_kernel<CBF16, MT, false>;
     hipLaunchKernelGGL(kernel, dim3(parts ? parts : strips), dim3(64 * SK_WAVES), 0, s, a, parts);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && parts) {
-        hipLaunchKernelGGL(gemm_few_join_kernel, dim3(strips, (a.M * (SK_COLS / 4) + 255) / 256), dim3(256), 0, s, a, parts);
+        hipLaunchKernelGGL(gemm_few_join_kernel<CBF16>, dim3(strips, (a.M * (SK_COLS / 4) + 255) / 256), dim3(256), 0, s, a, parts);
         e = hipGetLastError();
     }
     return e;
 }
 
 // The tiled kernel (gemm_tile.h) on the columns up to n_end
-template <int BM, int BN, int ST, int KS>
-hipError_t launch_tiles(EArgs a, int n_end, hipStream_t s)
+template <int BM, int BN, int ST, int KS, bool CBF16>
+hipError_t launch_tiles(EArgs<CBF16> a, int n_end, hipStream_t s)
 {
     constexpr int MF = (BK / 32) % KS == 0 ? 16 : 32;
     a.tiles_n = (n_end - a.n_begin + BN - 1) / BN;
     a.n_tiles = (a.M + BM - 1) / BM * a.tiles_n;
     a.n_wg = a.n_tiles * a.n_split;
-    auto kernel = gemm_kernel<BM, BN, ST, KS, MF, false, false, EArgs>;
+    auto kernel = gemm_kernel<BM, BN, ST, KS, MF, false, false, EArgs<CBF16>>;
     if constexpr (BM == 128)
         if (a.n_split > 1)
-            kernel = gemm_kernel<BM, BN, ST, KS, MF, false, true, EArgs>;
+            kernel = gemm_kernel<BM, BN, ST, KS, MF, false, true, EArgs<CBF16>>;
     hipLaunchKernelGGL(kernel, dim3(a.n_wg), dim3(NT), 0, s, a);
     return hipGetLastError();
 }
@@ -452,7 +470,8 @@ size_t workspace_need(int M, int N, int K, int num_splits)
     return sp > 1 ? (size_t)sp * M * (N - choose(M, N, K, sp).n_256) * 4 : 0;
 }
 
-hipError_t launch(EArgs a, hipStream_t s)
+template <bool CBF16>
+hipError_t launch(EArgs<CBF16> a, hipStream_t s)
 {
     if (few(a.M)) {
         const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
@@ -465,7 +484,7 @@ hipError_t launch(EArgs a, hipStream_t s)
     a.n_split = std::min(a.n_split, (a.K + BK - 1) / BK);
     const Choice c = choose(a.M, a.N, a.K, a.n_split);
     if (c.n_256) {
-        EArgs first = a;
+        EArgs<CBF16> first = a;
         first.n_split = 1;
         e = launch_tiles<256, 256, 2, 1>(first, c.n_256, s);
         if (c.n_256 == a.N)
@@ -478,7 +497,7 @@ hipError_t launch(EArgs a, hipStream_t s)
     if (e != hipSuccess || a.n_split == 1)
         return e;
     const size_t threads = (size_t)a.M * (a.N - a.n_begin) / 4;
-    hipLaunchKernelGGL(gemm_join_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(gemm_join_kernel<CBF16>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -538,20 +557,22 @@ ta_status gemm_bf16_epilogue(const void *A, const void *B, const void *bias, con
             overlaps(workspace, w_bytes, residual, c_bytes))
             return TA_ERR_ALIASING;
     }
-    EArgs a = {};
-    a.A = (const uint16_t *)A;
-    a.B = (const uint16_t *)B;
-    a.C = workspace;
-    a.M = M;
-    a.N = N;
-    a.K = K;
-    a.n_split = num_splits;
-    a.bias = (const uint16_t *)bias;
-    a.R = residual;
-    a.out = C;
-    a.act = activation;
-    a.c_bf16 = c_bf16 != 0;
-    return launch(a, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+    GArgs p = {};
+    p.A = (const uint16_t *)A;
+    p.B = (const uint16_t *)B;
+    p.C = workspace;
+    p.M = M;
+    p.N = N;
+    p.K = K;
+    p.n_split = num_splits;
+    const auto run = [&](auto a) {
+        a.bias = (const uint16_t *)bias;
+        a.R = residual;
+        a.out = C;
+        a.act = activation;
+        return launch(a, (hipStream_t)stream);
+    };
+    return (c_bf16 ? run(EArgs<true>{p}) : run(EArgs<false>{p})) == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
 }
 
 ta_status gemm_epilogue_workspace_bytes(int M, int N, int K, int num_splits, size_t *bytes)
