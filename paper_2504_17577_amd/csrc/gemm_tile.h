@@ -88,6 +88,14 @@ __device__ __forceinline__ void dma16(uint32_t lds, uint32_t voff, u32x4s rsrc)
                  : "memory");
 }
 
+// What the lanes of a wave wrote to LDS before this, all of its lanes read after it (a
+// wave's LDS accesses are carried out in order: this keeps the compiler to the order)
+__device__ __forceinline__ void wave_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ uint32_t lds_addr(const void *p)
 {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
@@ -468,6 +476,8 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
             }
             if (KS > 1)
                 __syncthreads();
+            else
+                wave_exchange();   // (other lanes of this wave wrote what a lane reads)
 #pragma unroll 1
             for (int s = 0; s < RPW; s += U * RPI) {
                 const int r = r_first + lr + s;
@@ -490,6 +500,8 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
                     now = next;
                 }
             }
+            if (KS == 1 && ph + 1 < PH)
+                wave_exchange();   // read before the next phase's writes
         }
         return;
     }
