@@ -553,6 +553,11 @@ ta_status gemm_epilogue_workspace_bytes(int M, int N, int K, int num_splits, siz
  * would leave CUs without work.  No HIP call. */
 ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits);
 
+/* How many of the first columns of C gemm_bf16_epilogue computes in 256 x 256 tiles,
+ * whole rounds of one per CU, for tests and tools: 0 (the other kernels take them all)
+ * to N.  No HIP call. */
+ta_status gemm_epilogue_route(int M, int N, int K, int num_splits, int *large_columns);
+
 /*
  * ta_schedule — host-side tile schedule of attn_fwd, for tests and tools.
  * For the query tile `q_tile` (rows q_tile*BM .. q_tile*BM+BM-1, BM from

@@ -462,11 +462,14 @@ Choice choose(int M, int N, int K, int sp)
     return best;
 }
 
+// ranges are whole steps
+int ranges(int K, int num_splits) { return std::min(num_splits, (K + BK - 1) / BK); }
+
 size_t workspace_need(int M, int N, int K, int num_splits)
 {
     if (few(M))
         return (size_t)few_parts(N, K, num_splits) * 2 * M * SK_COLS * 4;
-    const int sp = std::min(num_splits, (K + BK - 1) / BK);   // ranges are whole steps
+    const int sp = ranges(K, num_splits);
     return sp > 1 ? (size_t)sp * M * (N - choose(M, N, K, sp).n_256) * 4 : 0;
 }
 
@@ -481,7 +484,7 @@ hipError_t launch(EArgs<CBF16> a, hipStream_t s)
                            : launch_few<4>(a, nt, s);
     }
     hipError_t e = hipSuccess;
-    a.n_split = std::min(a.n_split, (a.K + BK - 1) / BK);
+    a.n_split = ranges(a.K, a.n_split);
     const Choice c = choose(a.M, a.N, a.K, a.n_split);
     if (c.n_256) {
         EArgs<CBF16> first = a;
@@ -620,6 +623,19 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits)
             ++sp;
     }
     *num_splits = std::max(1, std::min(sp, std::min(steps / SK_WAVES, MAX_SPLITS)));
+    return TA_OK;
+}
+
+ta_status gemm_epilogue_route(int M, int N, int K, int num_splits, int *large_columns)
+{
+    if (!large_columns)
+        return TA_ERR_NULL_POINTER;
+    const ta_status rc = check_sizes(M, N, K);
+    if (rc != TA_OK)
+        return rc;
+    if (num_splits < 1 || num_splits > MAX_SPLITS)
+        return TA_ERR_INVALID_SHAPE;
+    *large_columns = few(M) ? 0 : choose(M, N, K, ranges(K, num_splits)).n_256;
     return TA_OK;
 }
 

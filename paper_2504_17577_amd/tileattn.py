@@ -120,6 +120,8 @@ def lib():
     L.gemm_epilogue_workspace_bytes.argtypes = [i, i, i, i, ctypes.POINTER(ctypes.c_size_t)]
     L.gemm_epilogue_plan.restype = i
     L.gemm_epilogue_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
+    L.gemm_epilogue_route.restype = i
+    L.gemm_epilogue_route.argtypes = [i, i, i, i, ctypes.POINTER(i)]
     L.ta_schedule.restype = i
     L.ta_schedule.argtypes = [i, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
     L.ta_tile_shape.restype = i
@@ -877,6 +879,14 @@ def gemm_epilogue_workspace_bytes(M: int, N: int, K: int, num_splits: int) -> in
 def gemm_epilogue_plan(M: int, N: int, K: int) -> int:
     n = ctypes.c_int()
     rc = lib().gemm_epilogue_plan(M, N, K, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
+def gemm_epilogue_route(M: int, N: int, K: int, num_splits: int) -> int:
+    n = ctypes.c_int()
+    rc = lib().gemm_epilogue_route(M, N, K, num_splits, ctypes.byref(n))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return n.value
