@@ -430,8 +430,8 @@ ta_status ssd_segment_heuristic(int batch, int seqlen, int nheads, int *num_segm
  *   K, V      device, bf16 [T, Hkv, D], read only: token t starts k_stride
  *             (v_stride) elements after token t - 1 (at least Hkv * D, at most
  *             2^30, a multiple of 8), so that they can be slices of a fused
- *             projection; 16-byte aligned.  T >= 1 and T * Hkv * D < 2^34
- *             (else TA_ERR_INVALID_SHAPE)
+ *             projection; 16-byte aligned.  T >= 1 and T * Hkv * D <= 2^34 -
+ *             1024 (else TA_ERR_INVALID_SHAPE)
  *   seq       device, int32 [T]: token t belongs to sequence seq[t]; NULL:
  *             token t belongs to sequence t (T <= B, else TA_ERR_INVALID_SHAPE)
  *   pos       device, int32 [T]: its position in that sequence.  A token whose
@@ -442,7 +442,7 @@ ta_status ssd_segment_heuristic(int batch, int seqlen, int nheads, int *num_segm
  * An 8-bit cache takes x / scale rounded to the nearest e4m3 number (to even),
  * beyond +-448 as +-448, infinities too; NaN stays NaN.  Of two tokens of one
  * call with the same place, which one it holds afterwards is not defined, piece
- * of 16 bytes by piece.  Caches must not overlap each other or an input
+ * of 8 elements by piece.  Caches must not overlap each other or an input
  * (TA_ERR_ALIASING).  Ownership, asynchrony and status codes as attn_fwd.
  */
 ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_t v_stride,

@@ -31,7 +31,7 @@ struct GArgs {
     const uint16_t *A, *B;
     void *C;
     int M, N, K;
-    int tiles_n;     // N / BN
+    int tiles_n;     // tiles in a row of C (of a launch's columns)
     int n_tiles;     // tiles of C
     int n_split;     // K ranges per tile; with more than one, C is fp32
                      // [n_split][M][N], one partial product per range
@@ -212,8 +212,8 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
         b_off[i] = (uint32_t)r * a.N * 2 + 16 * (EDGE ? min(ch, (a.N - n0) / 8 - 1) : ch);
     }
 
-    // this range's K steps (ranges of whole steps, as even as they go; K * N <
-    // 2^30 and N >= 128, so the products fit 32 bits)
+    // this range's K steps (ranges of whole steps, as even as they go; a step is 64 rows
+    // and there are at most 64 ranges, so the products are at most K + 63)
     const uint32_t kt_all = EDGE ? (a.K + BK - 1) / BK : a.K / BK;
     int kt_lo = 0, n_kt = kt_all;
     if (SPLIT) {
