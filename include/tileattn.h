@@ -501,7 +501,10 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
 /* Workspace bytes attn_decode_paged needs for num_parts (0 for none).  No HIP call. */
 ta_status attn_paged_workspace_bytes(int Hq, int Hkv, int D, int num_parts, size_t *bytes);
 
-/* A part count for attn_decode_paged, from the table's capacity.  No HIP call. */
+/* A part count for attn_decode_paged, from the table's capacity (the lengths are on the
+ * device).  A caller that knows all sequences to be short behind a large table takes 0
+ * instead: one workgroup a head and no second kernel (a sequence of 37 positions 4 us
+ * instead of 9.5, 32 of 200 9 instead of 14).  No HIP call. */
 ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages,
                           int *num_parts);
 

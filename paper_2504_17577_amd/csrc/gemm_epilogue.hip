@@ -477,6 +477,9 @@ template <bool CBF16>
 hipError_t launch(EArgs<CBF16> a, hipStream_t s)
 {
     if (few(a.M)) {
+        // Weights that the 256 MB Infinity Cache cannot hold: non-temporal.  us, ordinary |
+        // non-temporal: 470 MB (1 x 28672 x 8192) 81.4 | 74.7, 1 GB (24 x 65536 x 8192) 185 | 169;
+        // 117 MB (24 x 14336 x 4096) read again by every call 22.9 | 24.9, from HBM 27.4 | 26.2
         const bool nt = (size_t)a.K * a.N * 2 > ((size_t)256 << 20);
         return a.M <= 16   ? launch_few<1>(a, nt, s)
                : a.M <= 32 ? launch_few<2>(a, nt, s)

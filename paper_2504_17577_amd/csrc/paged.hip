@@ -900,13 +900,21 @@ ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_
         return TA_ERR_UNSUPPORTED;
     // Two workgroups per CU share the batch, unless the longest sequence the table
     // has room for is short enough for one workgroup a head, which needs no second
-    // kernel.  us, one a head | 512 parts (bf16, 128 dims, 32 query and 8 K/V heads):
-    // B=1 500 keys 8.8 | 9.8, 2000 keys 29 | 11; B=4 1000 keys 17 | 12.5 (and 4 us less
-    // of the host's time for one launch); B=64 to 1000 mixed 24 | 18; but
-    // B=128 (8-bit) to 800 mixed 17 | 23, B=128 16 heads of 64 dims 200 keys 21 | 28.
+    // kernel.  us on the GPU, one a head | 512 parts (bf16, 128 dims, 32 query and 8
+    // K/V heads; the second launch costs the host 4 us besides):
+    //   keys   300       500       640       768       900       1024
+    //   B=1    7.2|10.5  9.5|10.0  11.4|10.2 12.9|10.3 15.7|10.6 16.0|10.6
+    //   B=4    8.6|11.3  10.4|10.7 11.9|10.8 13.5|10.9 16.3|12.8 16.7|12.8
+    //   B=32   10.7|16.1 14.1|20.4 16.4|21.4 19.1|25.0 22.7|27.5 24.6|30.1
+    //   mixed to 500, 768 and 1000: B=64 12.3|16.3, 18.3|16.9, 19.8|18.7; B=128
+    //   19.8|23.9, 24.0|25.0, 28.5|27.0
     // Where heads are many for the longest sequence's length, its workgroup alone is
-    // not what the call waits for, and no share stops at each of many short heads:
-    // B=128 32 K/V heads of 64 dims to 2000 mixed 64 | 72.
+    // not what the call waits for, and no share stops at each of many short heads.
+    // Sequences and K/V heads, mixed to `cap` (64 dims with 32 heads, 128 with 8):
+    //   heads >= 2 cap: 64 x 32 to 1024 22.9|33.1, 128 x 32 to 2048 60.5|79.1, 256 x 32 to
+    //   4096 194|199, 256 x 8 to 1024 44.3|46.2, 512 x 8 to 2048 116|123
+    //   = cap: 64 x 32 to 2048 41.9|41.2, 128 x 32 to 4096 116|117, 256 x 8 to 2048 70|62
+    //   = cap / 2: 64 x 32 to 4096 72.9|58.4, 128 x 8 to 2048 56.4|36.6
     const int64_t cap = (int64_t)max_pages * page_size;
     const int64_t heads = (int64_t)B * Hkv * paged_row_blocks(Hq / Hkv);
     *num_parts = cap <= 768 || (cap <= 1024 && heads >= 1024) || heads >= 2 * cap ? 0 : 512;

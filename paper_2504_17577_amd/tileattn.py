@@ -824,7 +824,8 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
     scales as kv_cache_append takes them.  ``scale`` defaults to 1/sqrt(D),
     ``out_dtype`` is torch.float32 (default) or torch.bfloat16.  A sequence of
     length 0 gets O = 0 and LSE = -inf.  The batch's positions are divided over
-    ``num_parts`` workgroups (default attn_paged_plan); ``workspace``, a uint8 GPU
+    ``num_parts`` workgroups (default attn_paged_plan, from the table's capacity; 0,
+    one a head, is faster for short sequences behind a large table); ``workspace``, a uint8 GPU
     tensor of at least attn_paged_workspace_bytes(...) bytes, is allocated here if
     needed and not given; it must stay alive until the launch has finished on
     ``stream``."""
