@@ -49,8 +49,9 @@ __device__ __forceinline__ float e4m3_arg(float x, float s)
 // One thread moves 8 elements (16 bytes) of a token's K or V row: thread i of
 // a token takes chunk i of its 2 Hkv D / 8, K first.  HBM bounds a prefill (16384
 // tokens of 8 heads of 128 dims, 134 MB read and written: 30.6 us, 4.4 TB/s of the
-// 4.8 that a copy of 4 GiB reaches; with the ordinary cache policy 34), latency a
-// decode step (3 us for 32 tokens).
+// 4.8 that a copy of 4 GiB reaches; with the ordinary cache policy 34), the loads one
+// behind the other (seq and pos, the table, then K or V and the scale) less: 32 tokens
+// 3 us, 2047 into 8 bits 6.5 us (2.6 at the copy's rate).
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
@@ -240,8 +241,10 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 //    the pages of the next K waited for all of V: 106 us became 139 for B=8 Sk=8191
 //    with one workgroup a head).
 // Measured, kernel without the merge (32 query and 8 K/V heads of 128 dims): B=8
-// Sk=8191 43 us (6.3 TB/s), 64 sequences of up to 16384 mixed, in pages of 16, 75
-// us (6.3 TB/s), B=1 Sk=100001 of 8 bits 35.5 us (5.8 TB/s).
+// Sk=8191 43-45 us (6.0-6.3 TB/s), 64 sequences of up to 16384 mixed, in pages of 16,
+// 75-78 us (6.0-6.3 TB/s), B=1 Sk=100001 of 8 bits 36 us (5.7 TB/s); of 8 bits and 64
+// dims (16 x 32 heads, 2001 positions) 31 us (4.3 TB/s: a wave's 32 keys are a quarter
+// of the bytes in flight, and the softmax's work per key is the same).
 template <int D, bool E4M3, int RT>
 __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
@@ -496,9 +499,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             for (int kp = 0; kp < KB / 2; ++kp) {
                 // The weights as three bf16 numbers that add up to all their 24 bits: with
                 // two, cut off, a bf16 O was not the nearest number to the exact one in 215
-                // of 32768 places (B=8 Sk=8191; 25 with an fp32 softmax by itself).  The
-                // loads leave the matrix cores the time: 49 us with two and with three, 8
-                // sequences of 8000 with 32 query heads to a K/V head 26.8 and 27.4
+                // of 32768 places (B=8 Sk=8191), with three it is not in 8.  The loads leave
+                // the matrix cores the time: 49 us with two and with three, 8 sequences of
+                // 8000 with 32 query heads to a K/V head 26.8 and 27.4
                 bf16x8 p[RT][3];
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {

@@ -53,6 +53,8 @@ CASES = [
     ([100001], 4, 2, 128, 64, (None, 511)),
     ([8191, 8192, 8193, 4095, 64, 63, 65, 0, 1], 20, 2, 64, 16, (None, 0, 100)),
     ([7 * i % 330 for i in range(700)], 4, 2, 128, 16, (None, 0, 512, 4096)),
+    ([64, 1, 63, 64, 0, 49], 3, 2, 64, 16, (None, 0, 1, 5)),       # as long as the table has room for
+    ([2048, 2048], 33, 1, 128, 1024, (None, 0, 2)),
 ]
 
 
