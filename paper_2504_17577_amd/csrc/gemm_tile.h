@@ -462,6 +462,8 @@ __global__ __launch_bounds__(NT, 2) void gemm_kernel(Args args)
             __syncthreads();   // every wave is done with the stage buffers
 #pragma unroll
         for (int ph = 0; ph < PH; ++ph) {
+            if (KS > 1)
+                wave_exchange();   // (the other groups' sums read before their place is written)
             if (kg == 0) {
 #pragma unroll
                 for (int i = 0; i < FP; ++i)
