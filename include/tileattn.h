@@ -498,6 +498,93 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
                             int num_parts, void *workspace, size_t workspace_bytes,
                             void *stream);
 
+/* What a paged cache holds, for the calls that take cache_type */
+typedef enum {
+    TA_CACHE_BF16 = 0,
+    TA_CACHE_E4M3 = 1,
+    TA_CACHE_MXFP4 = 2
+} ta_cache_type;
+
+/*
+ * 4-bit numbers (MXFP4 of the OCP microscaling formats), in caches and weights: rows of
+ * n elements (n % 32 == 0) are n / 2 bytes of codes and n / 32 bytes of scales.  A code
+ * is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1); element 2 i of a row is in the
+ * low half of byte i, element 2 i + 1 in the high half.  Scale byte e multiplies 32
+ * elements by 2^(e - 127); e = 255 makes them NaN.
+ *
+ * A 4-bit paged cache is laid out as the others are: codes, uint8
+ * [num_pages, Hkv, page_size, D / 2], and scales, uint8 [num_pages, Hkv, page_size,
+ * D / 32], for K and for V; all 16-byte aligned.
+ */
+
+/*
+ * qk_norm_rope_append — from the projection to the cache in one pass: norm of the new
+ * tokens' queries and keys, head by head, their position rotation, and the append of
+ * keys and values to the paged cache.
+ *
+ *   n(x) = x / sqrt(mean(x^2) + eps) * w      where a weight w is given, else x
+ *   y    = R(pos) n(x): of the first rot_dim dims each pair (a, b) becomes
+ *          (a cos - b sin, b cos + a sin), the others stay
+ *   Q_out[t,h,:] = y of Q[t,h,:];  K_cache takes y of K[t,h,:], V_cache V[t,h,:] itself
+ *
+ *   Q, K, V   device, bf16 [T, Hq, D] and [T, Hkv, D], read only, with strides between
+ *             tokens as kv_cache_append takes them; 16-byte aligned.  Hq 0..65536 (0: Q,
+ *             Q_out and q_weight are not looked at), any Hkv >= 1 beside it; 1 <= T < 2^24
+ *   q_weight, k_weight  device, bf16 [D], or NULL for no norm; 16-byte aligned
+ *   eps       >= 0, finite (else TA_ERR_INVALID_SCALE)
+ *   cos_sin   device, fp32 [num_positions, rot_dim], 16-byte aligned: for position p and
+ *             pair i the cosine at [p][i] and the sine at [p][rot_dim / 2 + i].  NULL,
+ *             with num_positions = rot_dim = 0: no rotation
+ *   rot_dim   16..D in steps of 16 (else TA_ERR_UNSUPPORTED)
+ *   interleaved  0: pair i is dims (i, rot_dim / 2 + i); else dims (2 i, 2 i + 1)
+ *   seq, pos  as kv_cache_append takes them: pos is the token's row of cos_sin too
+ *   Q_out     device, bf16 [T, Hq, D], contiguous, 16-byte aligned        written
+ *   cache_type  a ta_cache_type (else TA_ERR_UNSUPPORTED)
+ *   k_scale, v_scale  bf16: NULL; e4m3: fp32 [Hkv] or NULL, read; MXFP4: the caches'
+ *             scale bytes, written with the codes, not NULL
+ *
+ * Which tokens the cache takes, and two of one place: as kv_cache_append (for MXFP4 the
+ * pieces are of 32 elements' codes and of their scale: such a place may end up with
+ * the codes of one and the scale of the other).  A token whose
+ * position is negative (padding) has zeros in Q_out; one whose position is
+ * num_positions or more has NaN there and is left out of the cache.  A token that the
+ * cache has no place for has its queries all the same.
+ *
+ * Queries, and keys for a bf16 cache, are computed in fp32 and rounded once, to nearest
+ * even.  Keys for 8 and 4 bits are computed in fp64, rounded to fp32 and then to the
+ * cache's type; e4m3 as kv_cache_append does.  MXFP4: the scale is the power of two that
+ * puts a group's largest number between 3.5 and 7 (at least 2^-126, at most 2^125), the
+ * codes are the nearest (to even), beyond 6 as 6, infinities too; a NaN makes its
+ * group's scale 255 and its codes 0.  Q_out, the caches and their written scales must
+ * not overlap each other or an input (TA_ERR_ALIASING).  Ownership, asynchrony and
+ * status codes as attn_fwd.
+ */
+ta_status qk_norm_rope_append(const void *Q, const void *K, const void *V, int64_t q_stride, int64_t k_stride,
+                              int64_t v_stride, const void *q_weight, const void *k_weight, float eps,
+                              const float *cos_sin, int num_positions, int rot_dim, int interleaved,
+                              const int *seq, const int *pos, void *Q_out, void *K_cache, void *V_cache,
+                              int cache_type, void *k_scale, void *v_scale, const int *page_table, int T,
+                              int B, int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                              void *stream);
+
+/*
+ * attn_decode_paged_mxfp4 — attn_decode_paged over a cache held in 4 bits.
+ *
+ *   K_cache, V_cache  device, codes, uint8 [num_pages, Hkv, page_size, D / 2]
+ *   k_scale, v_scale  device, scales, uint8 [num_pages, Hkv, page_size, D / 32],
+ *                     16-byte aligned, not NULL
+ * Everything else as attn_decode_paged, with its plan and its workspace: keys and values
+ * enter the products as the numbers they stand for, exactly (those past the largest bf16
+ * number as infinity); a scale of 255 within a sequence's positions makes what it enters
+ * NaN.
+ */
+ta_status attn_decode_paged_mxfp4(const void *Q, int64_t q_stride, const void *K_cache,
+                                  const void *V_cache, const void *k_scale, const void *v_scale,
+                                  const int *page_table, const int *seq_lens, void *O, int o_bf16,
+                                  float *LSE, int B, int Hq, int Hkv, int D, int num_pages,
+                                  int page_size, int max_pages, float scale, int num_parts,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
 /* Workspace bytes attn_decode_paged needs for num_parts (0 for none).  No HIP call. */
 ta_status attn_paged_workspace_bytes(int Hq, int Hkv, int D, int num_parts, size_t *bytes);
 

@@ -1,10 +1,12 @@
 // Paged key/value cache for gfx950 (MI355X): new tokens' K and V into the
 // pages (kv_cache_append), and attention of one new token per sequence over
-// them (attn_decode_paged).
+// them (attn_decode_paged, attn_decode_paged_mxfp4).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
+#include "cache_checks.h"
+#include "mxfp4.h"
 #include "paged_plan.h"
 #include "tileattn.h"
 
@@ -97,7 +99,8 @@ struct PagedArgs {
     const uint16_t *Q;
     int64_t q_stride;
     const void *K, *V;
-    const float *ks, *vs;
+    const float *ks, *vs;      // per K/V head; MXFP4: none, and the scales' bytes
+    const uint8_t *kx, *vx;
     const int *table, *lens;
     void *O;
     float *LSE, *W;
@@ -245,16 +248,18 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 // 75-78 us (6.0-6.3 TB/s), B=1 Sk=100001 of 8 bits 36 us (5.7 TB/s); of 8 bits and 64
 // dims (16 x 32 heads, 2001 positions) 31 us (4.3 TB/s: a wave's 32 keys are a quarter
 // of the bytes in flight, and the softmax's work per key is the same).
-template <int D, bool E4M3, int RT>
+template <int D, int TYPE, int RT>
 __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
-    constexpr int KB = 2;                        // 16-key blocks per wave and step
+    constexpr bool E4M3 = TYPE == TA_CACHE_E4M3, MX = TYPE == TA_CACHE_MXFP4;
+    constexpr int KB = MX && RT == 1 ? 4 : 2;    // 16-key blocks per wave and step
     constexpr int KS = 16 * KB;
     constexpr int KK = D / 32;                   // k-steps of the scores
-    constexpr int ROW = D * (E4M3 ? 1 : 2);      // bytes of a key
-    constexpr int KL = ROW / 64;                 // 16-byte loads per lane and key block
+    constexpr int ROW = MX ? D / 2 : D * (E4M3 ? 1 : 2);   // bytes of a key
+    constexpr int KL = MX ? 1 : ROW / 64;        // loads of up to 16 bytes per lane and key block
     constexpr int DJ = D / 16;                   // dims of a value per lane
-    constexpr int VW = DJ * (E4M3 ? 1 : 2) / 4;  // dwords of them
+    constexpr int VW = MX ? 1 : DJ * (E4M3 ? 1 : 2) / 4;   // dwords of them
+    constexpr int XG = D / 32;                   // MXFP4: scales of a key
     __shared__ __attribute__((aligned(16))) float po[NW][16 * RT][D];
     __shared__ float ml[NW][2][16 * RT];
 
@@ -312,7 +317,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 #pragma unroll
             for (int kk = 0; kk < KK; ++kk)
                 q[i][kk] = __builtin_bit_cast(
-                    bf16x8, *(const u32x4 *)(qp + (E4M3 ? 64 * (kk >> 1) + 16 * g + 8 * (kk & 1) : 32 * kk + 8 * g)));
+                    bf16x8, *(const u32x4 *)(qp + (MX     ? D / 4 * g + 8 * kk
+                                               : E4M3 ? 64 * (kk >> 1) + 16 * g + 8 * (kk & 1)
+                                                      : 32 * kk + 8 * g)));
         }
         const float c = a.c * (a.ks ? a.ks[h] : 1.f);
 
@@ -336,7 +343,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             for (int kb = 0; kb < KB; ++kb)
                 page[kb] = table[min(((first + s * KS) >> 4) + kb, last_block) >> (a.page_shift - 4)];
         };
-        size_t at[KB];
+        size_t at[KB];             // (MXFP4: the rows before it)
         bool bad[KB], next_bad[KB];
         auto place = [&](int s) {
 #pragma unroll
@@ -344,17 +351,27 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 const int pg = paged_checked(page[kb], a.num_pages);
                 const int blk = min(((first + s * KS) >> 4) + kb, last_block);
                 const int in = (blk << 4) & ((1 << a.page_shift) - 1);
-                at[kb] = ((((size_t)max(pg, 0) * a.Hkv + h) << a.page_shift) + in) * ROW;
+                at[kb] = ((((size_t)max(pg, 0) * a.Hkv + h) << a.page_shift) + in) * (MX ? 1 : ROW);
                 next_bad[kb] = pg < 0;
             }
         };
         u32x4 kr[KB][KL];
         uint32_t vr[KB][4][VW];
+        uint32_t kx[KB], vx[KB];   // MXFP4: a key's scales
         auto load_k = [&]() {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const unsigned char *p = (const unsigned char *)a.K + at[kb];
-                if constexpr (KL == 1) {
+                const unsigned char *p = (const unsigned char *)a.K + at[kb] * (MX ? ROW : 1);
+                if constexpr (MX) {        // row c16, dims D / 4 g .. of it, one group's
+                    const unsigned char *e = p + (uint32_t)(c16 * ROW + D / 8 * g);
+                    if constexpr (D == 128) {
+                        kr[kb][0] = __builtin_nontemporal_load((const u32x4 *)e);
+                    } else {
+                        const u32x2 x = __builtin_nontemporal_load((const u32x2 *)e);
+                        kr[kb][0] = u32x4{x[0], x[1], 0, 0};
+                    }
+                    kx[kb] = __builtin_nontemporal_load(a.kx + at[kb] * XG + (uint32_t)(c16 * XG + D / 4 * g / 32));
+                } else if constexpr (KL == 1) {
                     kr[kb][0] = __builtin_nontemporal_load((const u32x4 *)(p + (uint32_t)(c16 * ROW + 16 * g)));
                 } else {
 #pragma unroll
@@ -367,11 +384,18 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
         auto load_v = [&]() {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
-                const unsigned char *p = (const unsigned char *)a.V + at[kb];
+                const unsigned char *p = (const unsigned char *)a.V + at[kb] * (MX ? ROW : 1);
+                if constexpr (MX) {        // all scales of key 4 g + c16 % 4
+                    const unsigned char *e = a.vx + at[kb] * XG + (uint32_t)((4 * g + (c16 & 3)) * XG);
+                    vx[kb] = D == 128 ? __builtin_nontemporal_load((const uint32_t *)e)
+                                      : __builtin_nontemporal_load((const uint16_t *)e);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const unsigned char *e = p + (uint32_t)((4 * g + i) * ROW + c16 * (4 * VW));
-                    if constexpr (VW == 4) {
+                    const unsigned char *e = p + (uint32_t)((4 * g + i) * ROW + c16 * (DJ * ROW / D));
+                    if constexpr (MX && D == 64) {
+                        vr[kb][i][0] = __builtin_nontemporal_load((const uint16_t *)e);
+                    } else if constexpr (VW == 4) {
                         const u32x4 x = __builtin_nontemporal_load((const u32x4 *)e);
 #pragma unroll
                         for (int w = 0; w < 4; ++w)
@@ -423,7 +447,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 #pragma unroll
                     for (int kk = 0; kk < KK; ++kk) {
                         bf16x8 k;
-                        if constexpr (E4M3) {
+                        if constexpr (MX) {
+                            k = tileattn_mx::eight(kr[kb][0][kk], tileattn_mx::scale_of(kx[kb]));
+                        } else if constexpr (E4M3) {
                             const uint32_t w0 = kr[kb][kk >> 1][2 * (kk & 1)], w1 = kr[kb][kk >> 1][2 * (kk & 1) + 1];
                             k = __builtin_bit_cast(bf16x8, u32x4{e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
                                                                  e4m3_bf16<false>(w1), e4m3_bf16<true>(w1)});
@@ -452,7 +478,24 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 
             // V as the A operand of O^T: k-slot of lane group g <-> keys 32 kp + 4 g
             // + (0..3) and 32 kp + 16 + 4 g + (0..3), as the scores left the weights
+            float vsc[KB][4];   // MXFP4: the scales of this lane's dims of its keys, from four lanes
+            if constexpr (MX) {
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) {
+                    const int x = (int)(((vx[kb] >> (8 * (c16 * XG / 16))) & 0xFF) << 23);
+                    vsc[kb][0] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0x00, 0xF, 0xF, true));
+                    vsc[kb][1] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0x55, 0xF, 0xF, true));
+                    vsc[kb][2] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0xAA, 0xF, 0xF, true));
+                    vsc[kb][3] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0xFF, 0xF, 0xF, true));
+                }
+            }
             if (tail) {   // what lies behind the last key may be anything
+                if constexpr (MX)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            vsc[kb][i] = key0 + 16 * kb + 4 * g + i < k_hi ? vsc[kb][i] : 1.f;
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -524,7 +567,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 #pragma unroll
                     for (int pr = 0; pr < 4; ++pr) {
                         const auto &e = vr[2 * kp + (pr >> 1)][2 * (pr & 1)], &o = vr[2 * kp + (pr >> 1)][2 * (pr & 1) + 1];
-                        if constexpr (E4M3) {
+                        if constexpr (MX) {
+                            const int kb = 2 * kp + (pr >> 1), i0 = 2 * (pr & 1);
+                            const uint32_t e2 = tileattn_mx::pair_at(e[0], vsc[kb][i0], j >> 1);
+                            const uint32_t o2 = tileattn_mx::pair_at(o[0], vsc[kb][i0 + 1], j >> 1);
+                            x0[pr] = low16(e2, o2);
+                            x1[pr] = high16(e2, o2);
+                        } else if constexpr (E4M3) {
                             // bytes j, j + 1 of both keys, paired by dim, then as bf16
                             const uint32_t w = __builtin_amdgcn_perm(o[j >> 2], e[j >> 2], j & 2 ? 0x07030602 : 0x05010400);
                             x0[pr] = e4m3_bf16<false>(w);
@@ -722,50 +771,87 @@ __global__ __launch_bounds__(MERGE_T) void attn_paged_merge_kernel(PagedArgs a, 
     }
 }
 
-bool misaligned(const void *p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
-
-struct Span {
-    const void *p;
-    size_t n;
-};
-
-bool overlaps(Span a, Span b)
-{
-    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-    return a.p && b.p && x < y + b.n && y < x + a.n;
-}
-
-// the sizes and types that both entry points check alike
-ta_status check_cache(int B, int Hkv, int D, int num_pages, int page_size, int max_pages, int cache_e4m3,
-                      const float *k_scale, const float *v_scale)
-{
-    if (B < 1 || Hkv < 1 || D < 1 || num_pages < 1 || page_size < 1 || max_pages < 1)
-        return TA_ERR_INVALID_SHAPE;
-    if ((D != 64 && D != 128) || page_size < 16 || (page_size & (page_size - 1)))
-        return TA_ERR_UNSUPPORTED;
-    if (!cache_e4m3 && (k_scale || v_scale))
-        return TA_ERR_UNSUPPORTED;
-    if ((int64_t)max_pages * page_size > 1ll << 30 || num_pages > 1 << 28 || Hkv > 1 << 16 ||
-        (int64_t)Hkv * page_size > 1ll << 30)
-        return TA_ERR_INVALID_SHAPE;
-    return TA_OK;
-}
-
-// elements of a cache: below 2^28 2^30 2^7 = 2^65 by the checks alone, so in 128 bits
-size_t cache_bytes(int Hkv, int D, int num_pages, int page_size, int cache_e4m3)
-{
-    const unsigned __int128 n = (unsigned __int128)num_pages * Hkv * page_size * D * (cache_e4m3 ? 1 : 2);
-    return n > (1ull << 62) ? (size_t)1 << 62 : (size_t)n;
-}
-
-bool heads_ok(int B, int Hq, int Hkv)
-{
-    return B >= 1 && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 && Hq <= 1 << 16 && (int64_t)B * Hq < 1ll << 24;
-}
-
 size_t workspace_need(int group, int D, int num_parts)
 {
     return (size_t)num_parts * 2 * paged_record(paged_block_rows(group), D) * 4;
+}
+
+template <int D>
+auto attention(int type, bool two)
+{
+    return type == TA_CACHE_BF16   ? (two ? attn_paged_kernel<D, TA_CACHE_BF16, 2> : attn_paged_kernel<D, TA_CACHE_BF16, 1>)
+           : type == TA_CACHE_E4M3 ? (two ? attn_paged_kernel<D, TA_CACHE_E4M3, 2> : attn_paged_kernel<D, TA_CACHE_E4M3, 1>)
+                                   : (two ? attn_paged_kernel<D, TA_CACHE_MXFP4, 2> : attn_paged_kernel<D, TA_CACHE_MXFP4, 1>);
+}
+
+ta_status attend(const void *Q, int64_t q_stride, const void *K_cache, const void *V_cache, int type,
+                 const void *k_scale, const void *v_scale, const int *page_table, const int *seq_lens, void *O,
+                 int o_bf16, float *LSE, int B, int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                 float scale, int num_parts, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!Q || !K_cache || !V_cache || !page_table || !seq_lens || !O || !LSE ||
+        (type == TA_CACHE_MXFP4 && (!k_scale || !v_scale)))
+        return TA_ERR_NULL_POINTER;
+    const ta_status rc = check_cache(B, Hkv, D, num_pages, page_size, max_pages, type, k_scale || v_scale);
+    if (rc != TA_OK)
+        return rc;
+    const bool mx = type == TA_CACHE_MXFP4;
+    const int64_t row = (int64_t)Hq * D;
+    if (!heads_ok(B, Hq, Hkv) || q_stride < row || q_stride % 8 || q_stride > 1ll << 30 || num_parts < 0 ||
+        num_parts > PAGED_MAX_PARTS)
+        return TA_ERR_INVALID_SHAPE;
+    const int group = Hq / Hkv, blocks = paged_row_blocks(group);
+    if (((int64_t)max_pages * page_size / PAGED_TILE + 1 + PAGED_HEAD) * B * Hkv * blocks >= 1ll << 31)   // tiles in 32 bits
+        return TA_ERR_INVALID_SHAPE;
+    if (misaligned(Q) || misaligned(K_cache) || misaligned(V_cache) || misaligned(O) || misaligned(LSE) ||
+        misaligned(page_table, 4) || misaligned(seq_lens, 4) || misaligned(k_scale, mx ? 16 : 4) ||
+        misaligned(v_scale, mx ? 16 : 4))
+        return TA_ERR_MISALIGNED;
+    if (!(scale >= 0.f) || !(scale <= 3.402823466e+38f))
+        return TA_ERR_INVALID_SCALE;
+    const size_t cb = cache_bytes(Hkv, num_pages, page_size, cache_row_bytes(D, type));
+    const size_t sb = scale_bytes(Hkv, D, num_pages, page_size, type);
+    const size_t need = workspace_need(group, D, num_parts);
+    const Span o = {O, (size_t)B * row * (o_bf16 ? 2 : 4)}, l = {LSE, (size_t)B * Hq * 4};
+    const Span w = {need ? workspace : nullptr, need};
+    const Span in[] = {{Q, (size_t)((B - 1) * q_stride + row) * 2}, {K_cache, cb}, {V_cache, cb},
+                       {page_table, (size_t)B * max_pages * 4}, {seq_lens, (size_t)B * 4},
+                       {k_scale, sb}, {v_scale, sb}};
+    if (overlaps(o, l))
+        return TA_ERR_ALIASING;
+    for (const Span &s : in)
+        if (overlaps(o, s) || overlaps(l, s))
+            return TA_ERR_ALIASING;
+    if (need) {
+        if (!workspace || workspace_bytes < need)
+            return TA_ERR_WORKSPACE;
+        if (misaligned(workspace))
+            return TA_ERR_MISALIGNED;
+        if (overlaps(w, o) || overlaps(w, l))
+            return TA_ERR_ALIASING;
+        for (const Span &s : in)
+            if (overlaps(w, s))
+                return TA_ERR_ALIASING;
+    }
+    const PagedArgs a = {(const uint16_t *)Q, q_stride, K_cache, V_cache, mx ? nullptr : (const float *)k_scale,
+                         mx ? nullptr : (const float *)v_scale, (const uint8_t *)k_scale, (const uint8_t *)v_scale,
+                         page_table, seq_lens, O,
+                         LSE, (float *)workspace, o_bf16 != 0, B, Hq, Hkv, num_pages, __builtin_ctz(page_size),
+                         max_pages, group, paged_block_rows(group), blocks, num_parts, scale * 1.44269504088896340736f};
+    const dim3 grid((unsigned)(num_parts ? num_parts : B * Hkv * blocks)), block(64 * NW);
+    hipStream_t s = (hipStream_t)stream;
+    const bool two = a.rows > 16;
+    const auto kernel = D == 64 ? attention<64>(type, two) : attention<128>(type, two);
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && num_parts) {
+        const auto merge = D == 64 ? attn_paged_merge_kernel<64> : attn_paged_merge_kernel<128>;
+        const int m_rows = min(a.rows, max(1, B * Hq / 512)), subs = (a.rows + m_rows - 1) / m_rows;
+        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks * subs)),
+                           dim3(B * Hq <= 128 ? MERGE_T : MERGE_T / 2), 0, s, a, m_rows);
+        e = hipGetLastError();
+    }
+    return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
 }
 
 }  // namespace
@@ -780,7 +866,8 @@ ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_
 {
     if (!K || !V || !pos || !K_cache || !V_cache || !page_table)
         return TA_ERR_NULL_POINTER;
-    const ta_status rc = check_cache(B, Hkv, D, num_pages, page_size, max_pages, cache_e4m3, k_scale, v_scale);
+    const int type = cache_e4m3 ? TA_CACHE_E4M3 : TA_CACHE_BF16;
+    const ta_status rc = check_cache(B, Hkv, D, num_pages, page_size, max_pages, type, k_scale || v_scale);
     if (rc != TA_OK)
         return rc;
     const int64_t row = (int64_t)Hkv * D;
@@ -791,7 +878,7 @@ ta_status kv_cache_append(const void *K, const void *V, int64_t k_stride, int64_
     if (misaligned(K) || misaligned(V) || misaligned(K_cache) || misaligned(V_cache) || misaligned(seq, 4) ||
         misaligned(pos, 4) || misaligned(page_table, 4) || misaligned(k_scale, 4) || misaligned(v_scale, 4))
         return TA_ERR_MISALIGNED;
-    const size_t cb = cache_bytes(Hkv, D, num_pages, page_size, cache_e4m3);
+    const size_t cb = cache_bytes(Hkv, num_pages, page_size, cache_row_bytes(D, type));
     const Span kc = {K_cache, cb}, vc = {V_cache, cb};
     const Span in[] = {{K, (size_t)((T - 1) * k_stride + row) * 2}, {V, (size_t)((T - 1) * v_stride + row) * 2},
                        {seq, (size_t)T * 4}, {pos, (size_t)T * 4}, {page_table, (size_t)B * max_pages * 4},
@@ -818,67 +905,21 @@ ta_status attn_decode_paged(const void *Q, int64_t q_stride, const void *K_cache
                             int num_pages, int page_size, int max_pages, float scale,
                             int num_parts, void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (!Q || !K_cache || !V_cache || !page_table || !seq_lens || !O || !LSE)
-        return TA_ERR_NULL_POINTER;
-    const ta_status rc = check_cache(B, Hkv, D, num_pages, page_size, max_pages, cache_e4m3, k_scale, v_scale);
-    if (rc != TA_OK)
-        return rc;
-    const int64_t row = (int64_t)Hq * D;
-    if (!heads_ok(B, Hq, Hkv) || q_stride < row || q_stride % 8 || q_stride > 1ll << 30 || num_parts < 0 ||
-        num_parts > PAGED_MAX_PARTS)
-        return TA_ERR_INVALID_SHAPE;
-    const int group = Hq / Hkv, blocks = paged_row_blocks(group);
-    if (((int64_t)max_pages * page_size / PAGED_TILE + 1 + PAGED_HEAD) * B * Hkv * blocks >= 1ll << 31)   // tiles in 32 bits
-        return TA_ERR_INVALID_SHAPE;
-    if (misaligned(Q) || misaligned(K_cache) || misaligned(V_cache) || misaligned(O) || misaligned(LSE) ||
-        misaligned(page_table, 4) || misaligned(seq_lens, 4) || misaligned(k_scale, 4) || misaligned(v_scale, 4))
-        return TA_ERR_MISALIGNED;
-    if (!(scale >= 0.f) || !(scale <= 3.402823466e+38f))
-        return TA_ERR_INVALID_SCALE;
-    const size_t cb = cache_bytes(Hkv, D, num_pages, page_size, cache_e4m3);
-    const size_t need = workspace_need(group, D, num_parts);
-    const Span o = {O, (size_t)B * row * (o_bf16 ? 2 : 4)}, l = {LSE, (size_t)B * Hq * 4};
-    const Span w = {need ? workspace : nullptr, need};
-    const Span in[] = {{Q, (size_t)((B - 1) * q_stride + row) * 2}, {K_cache, cb}, {V_cache, cb},
-                       {page_table, (size_t)B * max_pages * 4}, {seq_lens, (size_t)B * 4},
-                       {k_scale, (size_t)Hkv * 4}, {v_scale, (size_t)Hkv * 4}};
-    if (overlaps(o, l))
-        return TA_ERR_ALIASING;
-    for (const Span &s : in)
-        if (overlaps(o, s) || overlaps(l, s))
-            return TA_ERR_ALIASING;
-    if (need) {
-        if (!workspace || workspace_bytes < need)
-            return TA_ERR_WORKSPACE;
-        if (misaligned(workspace))
-            return TA_ERR_MISALIGNED;
-        if (overlaps(w, o) || overlaps(w, l))
-            return TA_ERR_ALIASING;
-        for (const Span &s : in)
-            if (overlaps(w, s))
-                return TA_ERR_ALIASING;
-    }
-    const PagedArgs a = {(const uint16_t *)Q, q_stride, K_cache, V_cache, k_scale, v_scale, page_table, seq_lens, O,
-                         LSE, (float *)workspace, o_bf16 != 0, B, Hq, Hkv, num_pages, __builtin_ctz(page_size),
-                         max_pages, group, paged_block_rows(group), blocks, num_parts, scale * 1.44269504088896340736f};
-    const dim3 grid((unsigned)(num_parts ? num_parts : B * Hkv * blocks)), block(64 * NW);
-    hipStream_t s = (hipStream_t)stream;
-    const bool two = a.rows > 16;
-    const auto kernel =
-        D == 64 ? (cache_e4m3 ? (two ? attn_paged_kernel<64, true, 2> : attn_paged_kernel<64, true, 1>)
-                              : (two ? attn_paged_kernel<64, false, 2> : attn_paged_kernel<64, false, 1>))
-                : (cache_e4m3 ? (two ? attn_paged_kernel<128, true, 2> : attn_paged_kernel<128, true, 1>)
-                              : (two ? attn_paged_kernel<128, false, 2> : attn_paged_kernel<128, false, 1>));
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && num_parts) {
-        const auto merge = D == 64 ? attn_paged_merge_kernel<64> : attn_paged_merge_kernel<128>;
-        const int m_rows = min(a.rows, max(1, B * Hq / 512)), subs = (a.rows + m_rows - 1) / m_rows;
-        hipLaunchKernelGGL(merge, dim3((unsigned)(B * Hkv * blocks * subs)),
-                           dim3(B * Hq <= 128 ? MERGE_T : MERGE_T / 2), 0, s, a, m_rows);
-        e = hipGetLastError();
-    }
-    return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+    return attend(Q, q_stride, K_cache, V_cache, cache_e4m3 ? TA_CACHE_E4M3 : TA_CACHE_BF16, k_scale, v_scale,
+                  page_table, seq_lens, O, o_bf16, LSE, B, Hq, Hkv, D, num_pages, page_size, max_pages, scale,
+                  num_parts, workspace, workspace_bytes, stream);
+}
+
+ta_status attn_decode_paged_mxfp4(const void *Q, int64_t q_stride, const void *K_cache,
+                                  const void *V_cache, const void *k_scale, const void *v_scale,
+                                  const int *page_table, const int *seq_lens, void *O, int o_bf16,
+                                  float *LSE, int B, int Hq, int Hkv, int D, int num_pages,
+                                  int page_size, int max_pages, float scale, int num_parts,
+                                  void *workspace, size_t workspace_bytes, void *stream)
+{
+    return attend(Q, q_stride, K_cache, V_cache, TA_CACHE_MXFP4, k_scale, v_scale, page_table, seq_lens, O, o_bf16,
+                  LSE, B, Hq, Hkv, D, num_pages, page_size, max_pages, scale, num_parts, workspace, workspace_bytes,
+                  stream);
 }
 
 ta_status attn_paged_workspace_bytes(int Hq, int Hkv, int D, int num_parts, size_t *bytes)

@@ -110,6 +110,12 @@ def lib():
     L.attn_decode_paged.restype = i
     L.attn_decode_paged.argtypes = ([p, ctypes.c_int64, p, p, i, p, p, p, p, p, i, p] + [i] * 7
                                     + [ctypes.c_float, i, p, ctypes.c_size_t, p])
+    L.qk_norm_rope_append.restype = i
+    L.qk_norm_rope_append.argtypes = ([p] * 3 + [ctypes.c_int64] * 3 + [p, p, ctypes.c_float, p, i, i, i] + [p] * 5
+                                      + [i, p, p, p] + [i] * 8 + [p])
+    L.attn_decode_paged_mxfp4.restype = i
+    L.attn_decode_paged_mxfp4.argtypes = ([p, ctypes.c_int64] + [p] * 7 + [i, p] + [i] * 7
+                                          + [ctypes.c_float, i, p, ctypes.c_size_t, p])
     L.attn_paged_workspace_bytes.restype = i
     L.attn_paged_workspace_bytes.argtypes = [i] * 4 + [ctypes.POINTER(ctypes.c_size_t)]
     L.attn_paged_plan.restype = i
@@ -741,18 +747,29 @@ def _vector(name, t, dtype, shape):
         raise TypeError(f"{name} must be a contiguous {dtype} GPU tensor of shape {tuple(shape)}")
 
 
+CACHE_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.uint8: 2} if torch else {}   # ta_cache_type
+E4M3, MXFP4 = 1, 2
+
+
 def _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table):
-    """(Hkv, D, num_pages, page_size, B, max_pages, e4m3) of a paged cache, checked."""
+    """(Hkv, D, num_pages, page_size, B, max_pages, type) of a paged cache, checked."""
     dtype = k_cache.dtype
-    e4m3 = dtype == torch.float8_e4m3fn
-    if k_cache.dim() != 4 or not (e4m3 or dtype == torch.bfloat16):
-        raise TypeError("k_cache must be a 4-D bfloat16 or float8_e4m3fn tensor [num_pages, Hkv, page_size, D]")
+    kind = CACHE_TYPES.get(dtype)
+    if k_cache.dim() != 4 or kind is None:
+        raise TypeError("k_cache must be a 4-D bfloat16 or float8_e4m3fn tensor [num_pages, Hkv, page_size, D], or "
+                        "a uint8 one [num_pages, Hkv, page_size, D / 2] of 4-bit numbers")
     shape = k_cache.shape
     num_pages, Hkv, page_size, D = shape
     _vector("k_cache", k_cache, dtype, shape)
     _vector("v_cache", v_cache, dtype, shape)
-    if k_scale is not None or v_scale is not None:
-        if not e4m3:
+    if kind == MXFP4:
+        D *= 2
+        if k_scale is None or v_scale is None:
+            raise TileAttnError(1, "a 4-bit cache needs k_scale and v_scale, uint8 [num_pages, Hkv, page_size, D / 32]")
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            _vector(name, t, torch.uint8, (num_pages, Hkv, page_size, D // 32))
+    elif k_scale is not None or v_scale is not None:
+        if kind != E4M3:
             raise TileAttnError(3, "k_scale and v_scale go with a float8_e4m3fn cache")
         for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
             if t is not None:
@@ -761,7 +778,7 @@ def _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table):
         raise TypeError("page_table must be 2-D [B, max_pages]")
     B, max_pages = table = page_table.shape
     _vector("page_table", page_table, torch.int32, table)
-    return Hkv, D, num_pages, page_size, B, max_pages, e4m3
+    return Hkv, D, num_pages, page_size, B, max_pages, kind
 
 
 def _ptr(t):
@@ -772,25 +789,81 @@ def kv_cache_append(k, v, k_cache, v_cache, page_table, pos, seq=None, k_scale=N
                     stream=None):
     """Writes new tokens' k, v [T, Hkv, D] (bf16; slices of a fused projection
     will do) into the paged caches [num_pages, Hkv, page_size, D] (bf16 or
-    float8_e4m3fn) at positions pos [T] of sequences seq [T] (default: token t of
-    sequence t); page_table [B, max_pages], pos and seq are int32 GPU tensors, the
+    float8_e4m3fn; or MXFP4: codes, uint8 [num_pages, Hkv, page_size, D / 2], with
+    uint8 k_scale and v_scale [num_pages, Hkv, page_size, D / 32], written too) at
+    positions pos [T] of sequences seq [T] (default: token t of sequence t);
+    page_table [B, max_pages], pos and seq are int32 GPU tensors, an 8-bit cache's
     scales fp32 [Hkv] (default 1).  Tokens with a negative position are left out.
     Returns (k_cache, v_cache)."""
-    Hkv, D, num_pages, page_size, B, max_pages, e4m3 = _paged_cache(k_cache, v_cache, k_scale, v_scale,
+    Hkv, D, num_pages, page_size, B, max_pages, kind = _paged_cache(k_cache, v_cache, k_scale, v_scale,
                                                                     page_table)
     T = k.shape[0]
     ks, vs = _rows("k", k, (T, Hkv, D)), _rows("v", v, (T, Hkv, D))
     _vector("pos", pos, torch.int32, (T,))
     if seq is not None:
         _vector("seq", seq, torch.int32, (T,))
+    if kind == MXFP4:
+        return _rope_append(None, k, v, None, k_cache, v_cache, page_table, pos, seq, k_scale, v_scale, None, None,
+                            0.0, None, False, 0, 0, ks, vs, T, 0, (Hkv, D, num_pages, page_size, B, max_pages, kind),
+                            stream)
     with _one_device(k, v, k_cache, v_cache, page_table, pos, seq, k_scale, v_scale):
         rc = lib().kv_cache_append(k.data_ptr(), v.data_ptr(), ks, vs, _ptr(seq), pos.data_ptr(),
-                                   k_cache.data_ptr(), v_cache.data_ptr(), int(e4m3), _ptr(k_scale),
+                                   k_cache.data_ptr(), v_cache.data_ptr(), int(kind == E4M3), _ptr(k_scale),
                                    _ptr(v_scale), page_table.data_ptr(), T, B, Hkv, D, num_pages,
                                    page_size, max_pages, _stream_handle(stream, k))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return k_cache, v_cache
+
+
+def _rope_append(q, k, v, out, k_cache, v_cache, page_table, pos, seq, k_scale, v_scale, q_weight, k_weight, eps,
+                 cos_sin, interleaved, rot, qs, ks, vs, T, Hq, cache, stream):
+    Hkv, D, num_pages, page_size, B, max_pages, kind = cache
+    with _one_device(k, q, v, out, k_cache, v_cache, page_table, pos, seq, k_scale, v_scale, q_weight, k_weight, cos_sin):
+        rc = lib().qk_norm_rope_append(
+            _ptr(q), k.data_ptr(), v.data_ptr(), qs, ks, vs, _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos_sin),
+            0 if cos_sin is None else cos_sin.shape[0], rot, int(bool(interleaved)), _ptr(seq), pos.data_ptr(),
+            _ptr(out), k_cache.data_ptr(), v_cache.data_ptr(), kind, _ptr(k_scale), _ptr(v_scale),
+            page_table.data_ptr(), T, B, Hq, Hkv, D, num_pages, page_size, max_pages, _stream_handle(stream, k))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return k_cache, v_cache
+
+
+def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, pos, cos_sin=None, q_weight=None, k_weight=None,
+                        eps: float = 1e-6, interleaved: bool = False, seq=None, k_scale=None, v_scale=None, out=None,
+                        stream=None):
+    """New tokens' q [T, Hq, D], k, v [T, Hkv, D] (bf16; slices of a fused projection
+    will do) on their way to attention: queries and keys normed per head (x /
+    sqrt(mean(x^2) + eps) times q_weight or k_weight [D] bf16, where given), rotated by
+    their position (where cos_sin is given), keys and values into the paged cache as
+    kv_cache_append puts them there, queries into ``out`` [T, Hq, D] (bf16).  cos_sin
+    [positions, rot_dim] (fp32) holds the cosines of a position's pairs, then their
+    sines; the first rot_dim dims of a head turn, pair i being dims (i, rot_dim / 2 + i)
+    or, ``interleaved``, (2 i, 2 i + 1).  A token with a negative position gets zeros in
+    ``out``, one past cos_sin's rows NaN; neither enters the cache.  Returns (out,
+    k_cache, v_cache)."""
+    cache = Hkv, D, _, _, _, _, _ = _paged_cache(k_cache, v_cache, k_scale, v_scale, page_table)
+    if q.dim() != 3:
+        raise TypeError("q must be a 3-D bfloat16 GPU tensor [T, Hq, D]")
+    T, Hq = q.shape[:2]
+    qs, ks, vs = _rows("q", q, (T, Hq, D)), _rows("k", k, (T, Hkv, D)), _rows("v", v, (T, Hkv, D))
+    _vector("pos", pos, torch.int32, (T,))
+    if seq is not None:
+        _vector("seq", seq, torch.int32, (T,))
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _vector(name, w, torch.bfloat16, (D,))
+    rot = 0
+    if cos_sin is not None:
+        if cos_sin.dim() != 2:
+            raise TypeError("cos_sin must be 2-D [positions, rot_dim]")
+        _vector("cos_sin", cos_sin, torch.float32, cos_sin.shape)
+        rot = cos_sin.shape[1]
+    out = _output("out", out, (T, Hq, D), torch.bfloat16, q)
+    _rope_append(q, k, v, out, k_cache, v_cache, page_table, pos, seq, k_scale, v_scale, q_weight, k_weight, float(eps),
+                 cos_sin, interleaved, rot, qs, ks, vs, T, Hq, cache, stream)
+    return out, k_cache, v_cache
 
 
 def attn_paged_workspace_bytes(Hq: int, Hkv: int, D: int, num_parts: int) -> int:
@@ -820,8 +893,8 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
                       workspace=None, out_dtype=None, stream=None):
     """O [B, Hq, D], LSE [B, Hq] (fp32) = attention of one new token per sequence,
     q [B, Hq, D] bf16 (a slice of a fused projection will do), over the first
-    seq_lens[b] (int32 GPU tensor [B]) positions of its pages; caches, table and
-    scales as kv_cache_append takes them.  ``scale`` defaults to 1/sqrt(D),
+    seq_lens[b] (int32 GPU tensor [B]) positions of its pages; caches (of 16, 8 or 4
+    bits), table and scales as kv_cache_append takes them.  ``scale`` defaults to 1/sqrt(D),
     ``out_dtype`` is torch.float32 (default) or torch.bfloat16.  A sequence of
     length 0 gets O = 0 and LSE = -inf.  The batch's positions are divided over
     ``num_parts`` workgroups (default attn_paged_plan, from the table's capacity; 0,
@@ -832,7 +905,7 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
     o_dtype = torch.float32 if out_dtype is None else out_dtype
     if o_dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
-    Hkv, D, num_pages, page_size, B, max_pages, e4m3 = _paged_cache(k_cache, v_cache, k_scale, v_scale,
+    Hkv, D, num_pages, page_size, B, max_pages, kind = _paged_cache(k_cache, v_cache, k_scale, v_scale,
                                                                     page_table)
     if q.dim() != 3:
         raise TypeError("q must be a 3-D bfloat16 GPU tensor [B, Hq, D]")
@@ -854,13 +927,11 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
           or not workspace.is_contiguous()):
         raise TypeError("workspace must be a contiguous uint8 GPU tensor")
     with _one_device(q, k_cache, v_cache, page_table, seq_lens, k_scale, v_scale, out, lse, workspace):
-        rc = lib().attn_decode_paged(q.data_ptr(), q_stride, k_cache.data_ptr(), v_cache.data_ptr(),
-                                     int(e4m3), _ptr(k_scale), _ptr(v_scale), page_table.data_ptr(),
-                                     seq_lens.data_ptr(), out.data_ptr(), int(o_dtype == torch.bfloat16),
-                                     lse.data_ptr(), B, Hq, Hkv, D, num_pages, page_size, max_pages,
-                                     float(scale), num_parts, _ptr(workspace),
-                                     workspace.numel() if workspace is not None else 0,
-                                     _stream_handle(stream, q))
+        call, kinds = (lib().attn_decode_paged_mxfp4, ()) if kind == MXFP4 else (lib().attn_decode_paged, (int(kind == E4M3),))
+        rc = call(q.data_ptr(), q_stride, k_cache.data_ptr(), v_cache.data_ptr(), *kinds, _ptr(k_scale), _ptr(v_scale),
+                  page_table.data_ptr(), seq_lens.data_ptr(), out.data_ptr(), int(o_dtype == torch.bfloat16),
+                  lse.data_ptr(), B, Hq, Hkv, D, num_pages, page_size, max_pages, float(scale), num_parts,
+                  _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream_handle(stream, q))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return out, lse
