@@ -649,6 +649,40 @@ ta_status gemm_epilogue_plan(int M, int N, int K, int *num_splits);
 ta_status gemm_epilogue_route(int M, int N, int K, int num_splits, int *large_columns);
 
 /*
+ * gemm_mxfp4_epilogue — C = act(A W^T + bias) + residual, for any number of rows, with
+ * the weights in 4 bits (MXFP4, described at qk_norm_rope_append).
+ *
+ *   A        device, bf16 [M, K] row-major                          read only
+ *   W        device, codes, uint8 [N, K / 2]: a row holds the weights of one output
+ *   W_scale  device, scales, uint8 [N, K / 32]; any alignment       read only
+ *   bias, residual, C, c_bf16, activation  as gemm_bf16_epilogue
+ *   N % 8 == 0 and K % 32 == 0 (else TA_ERR_UNSUPPORTED); sizes up to those of
+ *   gemm_bf16_epilogue; A, W, bias, residual, C and workspace 16-byte aligned; C apart
+ *   from A, W, W_scale and bias, and from residual unless it is C
+ *   num_splits  1..64 (else TA_ERR_INVALID_SHAPE): ranges of K that separate workgroups
+ *               sum, in whole steps of 128 (up to 64 rows: at most one for every eight
+ *               steps); for more than one, each range's fp32 product goes to
+ *               `workspace` (device, at least gemm_mxfp4_workspace_bytes(...) bytes, owned
+ *               by the caller, no overlap with any other argument; TA_ERR_WORKSPACE if
+ *               NULL or smaller) and a second kernel adds them in range order
+ *
+ * The weights enter the products as the numbers that they stand for, exactly (those past
+ * the largest bf16 number as infinity); a scale of 255 makes its row's column of C NaN.
+ * Sums, bias, activation and residual are fp32; a bf16 C is rounded once, to nearest
+ * even.  Ownership, asynchrony and status codes as gemm_bf16.
+ */
+ta_status gemm_mxfp4_epilogue(const void *A, const void *W, const void *W_scale, const void *bias,
+                              const void *residual, void *C, int c_bf16, int activation, int M,
+                              int N, int K, int num_splits, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Workspace bytes gemm_mxfp4_epilogue needs, 0 for one range.  No HIP call. */
+ta_status gemm_mxfp4_workspace_bytes(int M, int N, int K, int num_splits, size_t *bytes);
+
+/* A split count for gemm_mxfp4_epilogue.  No HIP call. */
+ta_status gemm_mxfp4_plan(int M, int N, int K, int *num_splits);
+
+/*
  * ta_schedule — host-side tile schedule of attn_fwd, for tests and tools.
  * For the query tile `q_tile` (rows q_tile*BM .. q_tile*BM+BM-1, BM from
  * ta_tile_shape) it reports how many key tiles of BN keys the kernel visits

@@ -128,6 +128,12 @@ def lib():
     L.gemm_epilogue_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
     L.gemm_epilogue_route.restype = i
     L.gemm_epilogue_route.argtypes = [i, i, i, i, ctypes.POINTER(i)]
+    L.gemm_mxfp4_epilogue.restype = i
+    L.gemm_mxfp4_epilogue.argtypes = [p] * 6 + [i] * 6 + [p, ctypes.c_size_t, p]
+    L.gemm_mxfp4_workspace_bytes.restype = i
+    L.gemm_mxfp4_workspace_bytes.argtypes = [i, i, i, i, ctypes.POINTER(ctypes.c_size_t)]
+    L.gemm_mxfp4_plan.restype = i
+    L.gemm_mxfp4_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
     L.ta_schedule.restype = i
     L.ta_schedule.argtypes = [i, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
     L.ta_tile_shape.restype = i
@@ -1013,6 +1019,79 @@ def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None,
         rc = lib().gemm_bf16_epilogue(a.data_ptr(), b.data_ptr(), _ptr(bias), _ptr(residual), out.data_ptr(),
                                       int(dt == torch.bfloat16), ACTIVATIONS[activation], M, N, K,
                                       num_splits, _ptr(ws), need, _stream_handle(stream, a))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return out
+
+
+def gemm_mxfp4_workspace_bytes(M: int, N: int, K: int, num_splits: int) -> int:
+    n = ctypes.c_size_t()
+    rc = lib().gemm_mxfp4_workspace_bytes(M, N, K, num_splits, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
+def gemm_mxfp4_plan(M: int, N: int, K: int) -> int:
+    n = ctypes.c_int()
+    rc = lib().gemm_mxfp4_plan(M, N, K, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _mxfp4_launch(M, N, K):
+    n = gemm_mxfp4_plan(M, N, K)
+    return n, gemm_mxfp4_workspace_bytes(M, N, K, n)
+
+
+def gemm_mxfp4_epilogue(a, w, w_scale, bias=None, activation: str = "none", residual=None, out=None,
+                        out_dtype=None, stream=None, num_splits: int | None = None):
+    """C = act(A W^T + bias) + residual for a contiguous bfloat16 GPU matrix a [M, K] (any
+    M) and weights in 4 bits (MXFP4: e2m1 codes w [N, K / 2], uint8, the first of two in
+    the low half, with a power of two for every 32 of a row, w_scale [N, K / 32], uint8;
+    N a multiple of 8, K of 32), bias [N] bf16; C and residual [M, N] are float32
+    (default) or bfloat16 (``out_dtype``).  ``activation``, ``out`` and ``num_splits``
+    (default gemm_mxfp4_plan) as gemm_bf16_epilogue takes them."""
+    if a.dtype != torch.bfloat16 or not a.is_cuda or a.dim() != 2 or not a.is_contiguous():
+        raise TypeError("a must be a contiguous 2-D bfloat16 GPU tensor")
+    M, K = a.shape
+    if K % 32:
+        raise TileAttnError(3, f"K must be a multiple of 32 (K={K})")
+    if w.dim() != 2:
+        raise TypeError("w must be a contiguous 2-D uint8 GPU tensor [N, K / 2]")
+    N = w.shape[0]
+    _vector("w", w, torch.uint8, (N, K // 2))
+    _vector("w_scale", w_scale, torch.uint8, (N, K // 32))
+    if N % 8:
+        raise TileAttnError(3, f"N must be a multiple of 8 (N={N})")
+    if activation not in ACTIVATIONS:
+        raise TileAttnError(3, f"activation {activation!r}: one of {', '.join(ACTIVATIONS)}")
+    dt = torch.float32 if out_dtype is None else out_dtype
+    if dt not in (torch.float32, torch.bfloat16):
+        raise TypeError("out_dtype must be torch.float32 or torch.bfloat16")
+    if bias is not None:
+        _vector("bias", bias, torch.bfloat16, (N,))
+    if residual is not None:
+        _vector("residual", residual, dt, (M, N))
+    out = _output("out", out, (M, N), dt, a)
+    chosen, ws = num_splits is None, None
+    if chosen:
+        num_splits, need = _mxfp4_launch(M, N, K)
+    else:
+        need = gemm_mxfp4_workspace_bytes(M, N, K, num_splits)
+    if need:
+        try:
+            ws = _workspace(need, a, stream)
+        except torch.OutOfMemoryError:
+            if not chosen:
+                raise
+            num_splits, need = 1, 0   # the caller asked for no workspace: one range needs none
+    with _one_device(a, w, w_scale, bias, residual, out):
+        rc = lib().gemm_mxfp4_epilogue(a.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _ptr(bias), _ptr(residual),
+                                       out.data_ptr(), int(dt == torch.bfloat16), ACTIVATIONS[activation], M, N, K,
+                                       num_splits, _ptr(ws), need, _stream_handle(stream, a))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return out

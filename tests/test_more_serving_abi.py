@@ -68,6 +68,46 @@ def test_attention_refusals(change, status):
     assert rc == status, f"{change}: got {ta.STATUS.get(rc, rc)}, want {ta.STATUS[status]}"
 
 
+A, W, S, BIAS, R, C = (0x100000000 * i for i in range(1, 7))
+GEMM = dict(A=A, W=W, S=S, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=4128, splits=2, ws=WS,
+            ws_bytes=1 << 20, stream=None)
+
+
+@no_gpu
+@pytest.mark.parametrize("change,status", [
+    (dict(A=0), 1), (dict(W=0), 1), (dict(S=0), 1), (dict(C=0), 1),
+    (dict(M=0), 2), (dict(N=0), 2), (dict(K=-32), 2), (dict(N=1 << 24), 2), (dict(K=1 << 22), 2),
+    (dict(M=1 << 20, N=1 << 15), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2), (dict(N=1 << 22, K=1 << 18), 2),
+    (dict(splits=0), 2), (dict(splits=65), 2), (dict(N=60), 3), (dict(K=4112), 3), (dict(act=-1), 3), (dict(act=5), 3),
+    (dict(A=A + 8), 4), (dict(W=W + 2), 4), (dict(C=C + 4), 4), (dict(bias=BIAS + 8), 4), (dict(R=R + 4), 4),
+    (dict(C=A + 16), 6), (dict(C=W + 16), 6), (dict(C=S), 6), (dict(S=C + 64 * 40 * 4 - 1), 6), (dict(C=BIAS), 6),
+    (dict(R=C + 16), 6), (dict(R=C - 16), 6),
+    (dict(ws=0), 8), (dict(ws_bytes=2 * 40 * 64 * 4 - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=A), 6), (dict(ws=W + 1024), 6),
+    (dict(ws=S + 16), 6), (dict(ws=C - 16), 6), (dict(ws=R), 6), (dict(ws=BIAS), 6),
+], ids=str)
+def test_gemm_refusals(change, status):
+    a = dict(GEMM, **change)
+    rc = ta.lib().gemm_mxfp4_epilogue(*a.values())
+    assert rc == status, f"{change}: got {ta.STATUS.get(rc, rc)}, want {ta.STATUS[status]}"
+
+
+def test_gemm_plan():
+    for M in (1, 16, 40, 65, 300, 4096):
+        for N in (8, 64, 1000, 4096, 65536):
+            for K in (32, 64, 992, 4096, 65536):
+                n = ta.gemm_mxfp4_plan(M, N, K)
+                assert 1 <= n <= 64 and ta.gemm_mxfp4_workspace_bytes(M, N, K, 1) == 0
+                assert ta.gemm_mxfp4_workspace_bytes(M, N, K, 64) % (4 * M * N) == 0
+    for bad in [(0, 8, 32), (1, 0, 32), (1, 8, -32), (1, 12, 32), (1, 8, 48), (1, 1 << 24, 32)]:
+        with pytest.raises(ta.TileAttnError):
+            ta.gemm_mxfp4_plan(*bad)
+        with pytest.raises(ta.TileAttnError):
+            ta.gemm_mxfp4_workspace_bytes(*bad, 2)
+    for splits in (0, 65):
+        with pytest.raises(ta.TileAttnError):
+            ta.gemm_mxfp4_workspace_bytes(1, 8, 32, splits)
+
+
 torch = pytest.importorskip("torch")
 BF16, U8, I32 = torch.bfloat16, torch.uint8, torch.int32
 
@@ -109,3 +149,17 @@ def test_append_and_attention_checks(gpu_like, change):  # noqa: F811
         ta.kv_cache_append(**dict(dict(k=kv, v=kv, **cache_args(), pos=torch.zeros(3, dtype=I32)), **change))
     with pytest.raises((TypeError, ta.TileAttnError)):
         ta.attn_decode_paged(**dict(dict(q=torch.zeros(3, 4, 64, dtype=BF16), **cache_args(), seq_lens=torch.zeros(3, dtype=I32)), **change))
+
+
+@pytest.mark.parametrize("change", [
+    dict(a=torch.zeros(4, 64)), dict(a=torch.zeros(4, 48, dtype=BF16)), dict(a=torch.zeros(64, 4, dtype=BF16).t()),
+    dict(w=torch.zeros(24, 32)), dict(w=torch.zeros(24, 31, dtype=U8)), dict(w=torch.zeros(32, 24, dtype=U8).t()),
+    dict(w=torch.zeros(24 * 32, dtype=U8)), dict(w_scale=torch.zeros(24, 2)), dict(w_scale=torch.zeros(24, 1, dtype=U8)),
+    dict(w=torch.zeros(20, 32, dtype=U8), w_scale=torch.zeros(20, 2, dtype=U8)), dict(bias=torch.zeros(24)),
+    dict(bias=torch.zeros(16, dtype=BF16)), dict(residual=torch.zeros(4, 24, dtype=BF16)),
+    dict(out=torch.zeros(4, 16)), dict(activation="tanh"), dict(out_dtype=torch.float16),
+], ids=str)
+def test_gemm_checks(gpu_like, change):  # noqa: F811
+    a = dict(a=torch.zeros(4, 64, dtype=BF16), w=torch.zeros(24, 32, dtype=U8), w_scale=torch.zeros(24, 2, dtype=U8))
+    with pytest.raises((TypeError, ta.TileAttnError)):
+        ta.gemm_mxfp4_epilogue(**dict(a, **change))
