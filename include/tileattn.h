@@ -683,6 +683,50 @@ ta_status gemm_mxfp4_workspace_bytes(int M, int N, int K, int num_splits, size_t
 ta_status gemm_mxfp4_plan(int M, int N, int K, int *num_splits);
 
 /*
+ * sample_logits — the next token of each row of logits, by temperature, top-k, top-p and
+ * min-p, from a given uniform number.
+ *
+ * Row b's tokens are in order by falling logit, those of equal logits by index.  With the
+ * weights w_i = exp((x_i - max x) / T), of that order are kept: the first top_k; of
+ * these each token before which there is less than top_p of their weight; each with
+ * w_i >= min_p; and the first in any case.  The token is the first, by index, up to which
+ * the kept tokens' weights sum to more than u of their whole sum, and logp the logarithm
+ * of its share of all tokens' weight: (x - max x) / T - ln sum_i w_i.
+ *
+ *   logits  device, fp32, or bf16 if l_bf16 != 0, [B, V]: row b starts stride elements
+ *           after row b - 1 (0 to 2^30); aligned to its type               read only
+ *   u       device, fp32 [B], 0 <= u < 1 (what is outside: as the nearest inside)
+ *   temperature  device, fp32 [B], or NULL for 1.  0, negative or NaN: the largest logit
+ *           (of several the first), whatever u and the filters, logp for T = 1; others are
+ *           taken as 1e-30 to 1e30
+ *   top_k   device, int32 [B], or NULL; 0, negative, or V and more: without
+ *   top_p   device, fp32 [B], or NULL; 1 and more: without; 0, negative or NaN: the first
+ *           alone
+ *   min_p   device, fp32 [B], or NULL; 0 and less: without; more than 1 or NaN: the first
+ *           alone
+ *   token   device, int32 [B]                                              written
+ *   logp    device, fp32 [B]                                               written
+ *   1 <= B <= 65536, 1 <= V <= 2^20 (else TA_ERR_INVALID_SHAPE); token and logp apart from
+ *   each other and every input (TA_ERR_ALIASING)
+ *   workspace  device, 16-byte aligned, at least sample_workspace_bytes(...) bytes, owned
+ *           by the caller, its contents on entry of no account, no overlap with any other
+ *           argument; TA_ERR_WORKSPACE if NULL or smaller
+ *
+ * A logit of -inf is never chosen.  A row with NaN or +inf in it, or with -inf only, has
+ * token -1 and logp NaN.  Weights are computed in fp64 and added exactly, as whole
+ * multiples of 2^-43 (a token of less than half of that is never chosen), so that results
+ * do not depend on the order of additions; logp's sum is in fp32 and fp64.  Ownership,
+ * asynchrony and status codes as attn_fwd.
+ */
+ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const float *u,
+                        const float *temperature, const int *top_k, const float *top_p,
+                        const float *min_p, int *token, float *logp, int B, int V,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace bytes sample_logits needs (0 for short rows and for many).  No HIP call. */
+ta_status sample_workspace_bytes(int B, int V, size_t *bytes);
+
+/*
  * ta_schedule — host-side tile schedule of attn_fwd, for tests and tools.
  * For the query tile `q_tile` (rows q_tile*BM .. q_tile*BM+BM-1, BM from
  * ta_tile_shape) it reports how many key tiles of BN keys the kernel visits

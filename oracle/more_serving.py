@@ -56,3 +56,41 @@ def norm_rope(x, pos, weight=None, eps=1e-6, cos_sin=None, interleaved=False):
         y[..., ia], y[..., ib] = a * c - b * s, b * c + a * s
         size[..., ia], size[..., ib] = np.abs(a * c) + np.abs(b * s), np.abs(b * c) + np.abs(a * s)
     return y, size
+
+
+def sample(x, u, temperature=1.0, top_k=0, top_p=np.inf, min_p=0.0, error=0.0):
+    """(tokens, logp of each) for one row of logits: the answer, or all of them that there
+    are if sums of weights are off by up to `error`."""
+    x = np.asarray(x, np.float64)
+    V = len(x)
+    best = x.max() if not np.isnan(x).any() else np.nan
+    if not np.isfinite(best):
+        return [-1], [np.nan]
+    greedy = not temperature > 0
+    T = 1.0 if greedy else min(max(float(temperature), 1e-30), 1e30)
+    w = np.exp((x - best) / T)
+    order = np.lexsort((np.arange(V), -(x + 0.0)))
+    ws = w[order]
+    k = 1 if greedy else min(V, top_k) if top_k > 0 else V
+    before = np.concatenate([[0.0], np.cumsum(ws)[:-1]])[:k]
+    total = ws[:k].sum()
+    u = min(max(float(u), 0.0), 1.0 - 2.0 ** -53)
+    tokens = set()
+
+    def kept(off):
+        keep = np.ones(k, bool)
+        if top_p < 1 or np.isnan(top_p):
+            keep &= before < top_p * total + off
+        if not min_p <= 0:
+            keep &= ws[:k] >= min_p - off
+        return max(1, int(keep.sum()))
+
+    low, high = (kept(-error), kept(error)) if error else (kept(0.0),) * 2
+    for n in range(low, high + 1):
+        some = np.sort(order[:n])
+        upto = np.cumsum(w[some])
+        last = int(np.searchsorted(upto, upto[-1]))      # (the last that counts)
+        at = [min(last, int(np.searchsorted(upto, u * upto[-1] + d, side="right"))) for d in (-error, error)]
+        tokens.update(int(t) for t in some[at[0]:at[1] + 1] if w[t] > 0)
+    tokens = sorted(tokens)
+    return tokens, [(x[t] - best) / T - np.log(w.sum()) for t in tokens]

@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SOURCES = [os.path.join(PKG, "csrc", n) for n in ("attn_fwd.hip", "mla_decode.hip", "gemm.hip", "ssd.hip",
                                                    "paged.hip", "gemm_epilogue.hip", "rope_append.hip",
-                                                   "gemm_mxfp4.hip")]
+                                                   "gemm_mxfp4.hip", "sample.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtileattn.so")
 

@@ -1,0 +1,1001 @@
+// The next token of each row of logits on gfx950 (MI355X): temperature, top-k, top-p,
+// min-p and the choice by a given uniform number (sample_logits).
+//
+// The order of a row is by logit, then by index, and every filter keeps a beginning of
+// it, so that all of them together come down to one place in the order.  The weights
+// exp((x - best) / T) and their sums decide at borders between tokens, so they are
+// computed in 64 bits and added as whole multiples of 2^-43: exactly, in any order.
+// What is less than half of that counts as nothing.
+//
+// Nothing is sorted.  A small top-k (this covers greedy rows) takes candidates:
+// the largest logits of a few thousand groups give a border that at least k tokens are
+// above and few more; those alone are weighed and compared, each with each.  Otherwise a histogram of the
+// weights over (best - x) / T, in 2047 buckets of 31 / 2048, finds the bucket in which
+// the place lies, and the tokens of that bucket alone are compared; should they be too
+// many (ties, most of all), their keys' range is narrowed in the same way.  The chosen
+// token is then found in the order of indexes, from the sums of slices of the row, in
+// one slice.
+//
+// A row is cut into slices for a few large rows: a kernel over slices for the largest
+// logit and the candidates, one over slices for the histograms (rows that need none
+// leave at once), and one over rows for the rest.  Many rows, or short ones, run the
+// three as one kernel, a workgroup a row.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "cache_checks.h"
+#include "even_parts.h"
+#include "tileattn.h"
+
+namespace {
+
+using namespace tileattn_detail;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned long long u64;
+
+constexpr int NT = 1024, NWAVE = NT / 64;
+constexpr int NB = 2048;                 // buckets; the last holds what counts as nothing
+constexpr double BUCKET = 31.0 / NB, PER_UNIT = NB / 31.0;
+constexpr double UNIT = 0x1p43;
+constexpr int LIST = 1024;               // tokens that are compared with each other, at most one a thread
+constexpr int CANDIDATES = 512;          // as many times the slices as a top-k may ask for to have candidates
+constexpr int GROUPS = 4;                // of a thread, whose largest logits set the border
+constexpr int SUBS = 1024;               // parts of a bucket's range of keys
+constexpr int MAX_SLICES = 32;
+constexpr int MAX_V = 1 << 20, MAX_B = 1 << 16;
+
+struct Slice {
+    float top;       // the slice's largest logit
+    int n;           // its candidates, or -1: the row takes the histogram
+    double z;        // sum of exp((x - top) / T); NaN if there is a NaN
+};
+
+struct SampleArgs {
+    const void *logits;
+    int64_t stride;
+    const float *u, *temperature;
+    const int *top_k;
+    const float *top_p, *min_p;
+    int *token;
+    float *logp;
+    int V, S;
+    // of slices, [row][slice]: records, candidates [LIST / S], weights and counts [NB]
+    Slice *slices;
+    u64 *lists, *weights;
+    uint32_t *counts;
+};
+
+struct __attribute__((aligned(16))) Token {
+    u64 place, w;
+};
+
+struct Shared {
+    Token list[LIST];
+    u64 w[2 * SUBS];
+    double table[NB];        // weight of a bucket's lower end, in units
+    u64 hist[NB];
+    uint32_t count[NB];
+    u64 scan[NWAVE], slice[MAX_SLICES], w_cut;
+    double z[NWAVE];
+    float best[NWAVE], low[NWAVE];
+    uint32_t n, lo, hi, at;
+    u64 cut;
+    int found;
+};
+
+// ---- the workgroup's sums ---------------------------------------------------
+
+template <class F, class Op>
+__device__ __forceinline__ F wave_all(F x, Op op)
+{
+#pragma unroll
+    for (int m = 32; m; m >>= 1)
+        x = op(x, __shfl_xor(x, m));
+    return x;
+}
+
+// op over all threads' x, through NWAVE places of LDS
+template <class F, class Op>
+__device__ __forceinline__ F block_all(F x, F *s, Op op)
+{
+    x = wave_all(x, op);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0)
+        s[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = s[0];
+#pragma unroll
+    for (int i = 1; i < NWAVE; ++i)
+        x = op(x, s[i]);
+    return x;
+}
+
+// The sum of the threads' x before this one; `all`: of all
+__device__ __forceinline__ u64 block_before(u64 x, u64 *s, u64 &all)
+{
+    u64 in = x;
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const u64 y = __shfl_up(in, d);
+        in += lane >= d ? y : 0;
+    }
+    __syncthreads();
+    if (lane == 63)
+        s[threadIdx.x / 64] = in;
+    __syncthreads();
+    u64 before = 0;
+    all = 0;
+#pragma unroll
+    for (int i = 0; i < NWAVE; ++i) {
+        before += i < (int)threadIdx.x / 64 ? s[i] : 0;
+        all += s[i];
+    }
+    return before + in - x;
+}
+
+// ---- a row -------------------------------------------------------------------
+
+// A row in chunks of 16 bytes from the 16-byte line that it begins in
+template <bool BF16>
+struct Row {
+    static constexpr int EPC = BF16 ? 8 : 4;
+    const unsigned char *line;
+    int off, V, chunks;      // elements before the row in its first chunk
+
+    __device__ __forceinline__ Row(const SampleArgs &a, int b)
+    {
+        const uintptr_t p = (uintptr_t)a.logits + (size_t)b * a.stride * (16 / EPC);
+        line = (const unsigned char *)(p & ~(uintptr_t)15);
+        off = (int)(p & 15) / (16 / EPC);
+        V = a.V;
+        chunks = (off + V + EPC - 1) / EPC;
+    }
+    __device__ __forceinline__ int index(int c, int e) const { return c * EPC + e - off; }
+    __device__ __forceinline__ float value(int i) const
+    {
+        if (BF16)
+            return __uint_as_float((uint32_t)((const uint16_t *)line)[i + off] << 16);
+        return ((const float *)line)[i + off];
+    }
+    // (the first and last chunk element by element: nothing outside the row is read; -inf
+    // stands there)
+    __device__ __forceinline__ u32x4 load(int c) const
+    {
+        if (c * EPC >= off && (c + 1) * EPC <= off + V)
+            return *(const u32x4 *)(line + (size_t)16 * c);
+        u32x4 x;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            x[w] = BF16 ? 0xFF80FF80u : 0xFF800000u;
+            if (BF16) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if ((unsigned)index(c, 2 * w + h) < (unsigned)V)
+                        x[w] = (x[w] & (h ? 0xFFFFu : 0xFFFF0000u)) |
+                               (uint32_t)((const uint16_t *)line)[c * EPC + 2 * w + h] << (16 * h);
+            } else if ((unsigned)index(c, w) < (unsigned)V) {
+                x[w] = ((const uint32_t *)line)[c * EPC + w];
+            }
+        }
+        return x;
+    }
+    static __device__ __forceinline__ float get(const u32x4 &x, int e)
+    {
+        if (BF16)
+            return __uint_as_float(e & 1 ? x[e >> 1] & 0xFFFF0000u : x[e >> 1] << 16);
+        return __uint_as_float(x[e]);
+    }
+    // f(chunk's number, its 16 bytes) for the chunks c0 .. c1, spread over the threads, U
+    // loads in flight
+    template <int U, class F>
+    __device__ __forceinline__ void each(int c0, int c1, F f) const
+    {
+        int c = c0 + threadIdx.x;
+        for (; c + (U - 1) * NT < c1; c += U * NT) {
+            u32x4 x[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                x[i] = load(c + i * NT);
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+                f(c + i * NT, x[i]);
+        }
+        for (; c < c1; c += NT)
+            f(c, load(c));
+    }
+};
+
+// What a row asks for
+struct Wish {
+    float T;
+    int k;           // V: no limit
+    bool few;        // candidates
+    double p, min_p;
+};
+
+__device__ __forceinline__ Wish wish_of(const SampleArgs &a, int b)
+{
+    Wish w = {1.f, a.V, false, INFINITY, 0.0};
+    if (a.top_k && a.top_k[b] > 0)
+        w.k = min(a.top_k[b], a.V);
+    if (a.top_p)
+        w.p = a.top_p[b];
+    if (a.min_p)
+        w.min_p = a.min_p[b];
+    if (a.temperature) {
+        const float t = a.temperature[b];
+        if (t > 0.f)
+            w.T = fminf(fmaxf(t, 1e-30f), 1e30f);
+        else
+            w.k = 1;                 // greedy
+    }
+    w.few = (int64_t)w.k * a.S <= CANDIDATES;
+    return w;
+}
+
+// Logits in an order of whole numbers, -0 as 0
+__device__ __forceinline__ uint32_t order_key(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+__device__ __forceinline__ u64 place_of(float x, int i) { return (u64)order_key(x) << 32 | (0xFFFFFFFFu - (uint32_t)i); }
+__device__ __forceinline__ int index_of(u64 place) { return (int)(0xFFFFFFFFu - (uint32_t)place); }
+__device__ __forceinline__ float logit_of(u64 place)
+{
+    const uint32_t k = (uint32_t)(place >> 32);
+    return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+
+// The bucket of a logit and its weight: exp(-d) = exp(-the bucket's lower end) exp(-r),
+// the second by its series (r < 0.0152: r^6 / 720 < 2^-45)
+struct Weigher {
+    double best, inv_T;
+    const double *table;
+
+    __device__ __forceinline__ int bucket(float x, double &r) const
+    {
+        const double d = (best - (double)x) * inv_T;
+        const int b = (int)fmin(d * PER_UNIT, (double)(NB - 1));
+        r = __builtin_fma((double)-b, BUCKET, d);
+        return b;
+    }
+    __device__ __forceinline__ int bucket(float x) const
+    {
+        double r;
+        return bucket(x, r);
+    }
+    static __device__ __forceinline__ double series(double r)
+    {
+        double p = __builtin_fma(r, -1.0 / 120, 1.0 / 24);
+        p = __builtin_fma(p, r, -1.0 / 6);
+        p = __builtin_fma(p, r, 0.5);
+        p = __builtin_fma(p, r, -1.0);
+        return __builtin_fma(p, r, 1.0);
+    }
+    // in units, exact to their fraction, and rounded
+    __device__ __forceinline__ double exact(float x) const
+    {
+        double r;
+        const int b = bucket(x, r);
+        return b == NB - 1 ? 0.0 : table[b] * series(r);
+    }
+    __device__ __forceinline__ u64 rounded(int b, double r) const
+    {
+        const double w = __builtin_fma(table[b], series(r), 0x1p52);
+        return (u64)__double_as_longlong(w) & 0xFFFFFFFFFFFFFull;
+    }
+    __device__ __forceinline__ u64 weight(float x) const
+    {
+        double r;
+        const int b = bucket(x, r);
+        return b == NB - 1 ? 0 : rounded(b, r);
+    }
+};
+
+__device__ __forceinline__ void fill_table(double *table)
+{
+    for (int i = threadIdx.x; i < NB; i += NT)
+        table[i] = exp(-i * BUCKET) * UNIT;
+}
+
+__device__ __forceinline__ Slice *slice_at(const SampleArgs &a, int b, int s) { return a.slices + (size_t)b * a.S + s; }
+
+// ---- 1: a slice's largest logit and candidates ------------------------------------
+
+template <bool BF16>
+__device__ Slice find_candidates(const SampleArgs &a, int b, int s, Shared &sm)
+{
+    const Row<BF16> row(a, b);
+    const Wish wish = wish_of(a, b);
+    const int c0 = even_begin(row.chunks, a.S, s), c1 = even_begin(row.chunks, a.S, s + 1);
+    float top[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+        top[i] = -INFINITY;
+    row.template each<GROUPS>(c0, c1, [&](int c, const u32x4 &x) {
+        float m = Row<BF16>::get(x, 0);
+#pragma unroll
+        for (int e = 1; e < Row<BF16>::EPC; ++e)
+            m = fmaxf(m, Row<BF16>::get(x, e));
+        const int g = (c - c0) / NT % GROUPS;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i)
+            top[i] = g == i ? fmaxf(top[i], m) : top[i];
+    });
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+        m = fmaxf(m, top[i]);
+    m = block_all(m, sm.best, [](float x, float y) { return fmaxf(x, y); });
+    Slice out = {m, -1, 0.0};
+    if (!wish.few || !(m < INFINITY))
+        return out;
+
+    // the border: the first of SUBS steps down to the lowest of the groups' largest that
+    // has k of them above it; if there are not k, whatever is not -inf
+    float low = INFINITY;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+        low = top[i] > -INFINITY ? fminf(low, top[i]) : low;
+    low = block_all(low, sm.low, [](float x, float y) { return fminf(x, y); });
+    const float range = m - low, step = range > 0.f && range < INFINITY ? (SUBS - 1) / range : 0.f;
+    auto level = [&](float x) { return (m - x) * step; };
+    for (int i = threadIdx.x; i < SUBS; i += NT)
+        sm.count[i] = 0;
+    if (threadIdx.x == 0) {
+        sm.n = 0;
+        sm.at = SUBS;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+        if (top[i] > -INFINITY)
+            atomicAdd(&sm.count[min((int)level(top[i]), SUBS - 1)], 1u);
+    __syncthreads();
+    static_assert(SUBS == NT, "one step per thread");
+    u64 all;
+    const u64 before = block_before(sm.count[threadIdx.x], sm.scan, all);
+    if (before < (u64)wish.k && before + sm.count[threadIdx.x] >= (u64)wish.k)
+        sm.at = threadIdx.x;
+    __syncthreads();
+    const float border = sm.at == SUBS ? INFINITY : (float)(sm.at + 1);
+    const int room = LIST / a.S;
+    const float base = m == -INFINITY ? 0.f : m, c2 = 1.44269504088896340736f / wish.T;
+    float z = 0.f;
+    row.template each<4>(c0, c1, [&](int c, const u32x4 &x) {
+        float cm = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < Row<BF16>::EPC; ++e) {
+            const float v = Row<BF16>::get(x, e);
+            cm = fmaxf(cm, v);
+            z += __builtin_amdgcn_exp2f((v - base) * c2);
+        }
+        if (cm > -INFINITY && (border == INFINITY || level(cm) < border))
+#pragma unroll
+            for (int e = 0; e < Row<BF16>::EPC; ++e) {
+                const float v = Row<BF16>::get(x, e);
+                if (v > -INFINITY && (border == INFINITY || level(v) < border)) {
+                    const uint32_t i = atomicAdd(&sm.n, 1u);
+                    if (i < (uint32_t)room)
+                        sm.list[i].place = place_of(v, row.index(c, e));
+                }
+            }
+    });
+    out.z = block_all((double)z, sm.z, [](double x, double y) { return x + y; });
+    out.n = sm.n <= (uint32_t)room ? (int)sm.n : -1;
+    return out;
+}
+
+// ---- 2: a slice's histogram ----------------------------------------------------------
+
+// sm.hist and, for a top-k, sm.count; NaN if there is one
+template <bool BF16>
+__device__ double fill_histogram(const SampleArgs &a, int b, int s, float best, Shared &sm)
+{
+    const Row<BF16> row(a, b);
+    const Wish wish = wish_of(a, b);
+    const int c0 = even_begin(row.chunks, a.S, s), c1 = even_begin(row.chunks, a.S, s + 1);
+    fill_table(sm.table);
+    for (int i = threadIdx.x; i < NB; i += NT) {
+        sm.hist[i] = 0;
+        sm.count[i] = 0;
+    }
+    if (threadIdx.x == 0)
+        sm.found = 0;
+    __syncthreads();
+    const Weigher weigh = {best, 1.0 / (double)wish.T, sm.table};
+    const bool counted = wish.k < a.V;
+    bool nan = false;
+    row.template each<2>(c0, c1, [&](int, const u32x4 &x) {
+#pragma unroll
+        for (int e = 0; e < Row<BF16>::EPC; ++e) {
+            const float v = Row<BF16>::get(x, e);
+            nan |= v != v;
+            double r;
+            const int i = weigh.bucket(v, r);
+            if (i < NB - 1) {
+                atomicAdd(&sm.hist[i], weigh.rounded(i, r));
+                if (counted)
+                    atomicAdd(&sm.count[i], 1u);
+            }
+        }
+    });
+    if (nan)
+        sm.found = 1;
+    __syncthreads();
+    return sm.found ? NAN : 0.0;
+}
+
+// ---- 3: the place in the order, and the token -----------------------------------------
+
+// A beginning of the order, of which a token is that `rank` tokens and `before` weight
+// lie above (the first, which nothing lies above, in any case)
+struct Border {
+    u64 k;           // tokens
+    double w;        // a token is in if less weight than this is before it
+    double least;    // and its own is not less than this
+    __device__ __forceinline__ bool in(u64 rank, u64 before, double own) const
+    {
+        return before == 0 || (rank < k && (double)before < w && own >= least);
+    }
+};
+
+// The list's tokens, each compared with each: P neighbouring threads (a power of two that
+// divides a wave) take one token, every P-th of the others each.
+struct Compared {
+    u64 rank, before;    // tokens and weight of the list above this thread's
+    u64 place, w;        // of it
+    bool own;            // one of the P threads, where there is a token
+};
+
+__device__ __forceinline__ int threads_each(int n)
+{
+    int p = 1;
+    while (p < 64 && 2 * p * n <= NT)
+        p *= 2;
+    return p;
+}
+
+__device__ Compared compare_list(Shared &sm, int n, const Weigher &weigh)
+{
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT)
+        sm.list[i].w = weigh.weight(logit_of(sm.list[i].place));
+    __syncthreads();
+    const int p = threads_each(n), i = threadIdx.x / p, part = threadIdx.x & (p - 1);
+    Compared t = {0, 0, 0, 0, i < n && part == 0};
+    if (i < n) {
+        const Token own = sm.list[i];
+        t.place = own.place;
+        t.w = own.w;
+        for (int j = part; j < n; j += p) {
+            const Token x = sm.list[j];
+            t.rank += x.place > own.place;
+            t.before += x.place > own.place ? x.w : 0;
+        }
+        for (int m = 1; m < p; m *= 2) {
+            t.rank += __shfl_xor(t.rank, m);
+            t.before += __shfl_xor(t.before, m);
+        }
+    }
+    return t;
+}
+
+__device__ __forceinline__ u64 block_sum(u64 x, Shared &sm)
+{
+    return block_all(x, sm.scan, [](u64 a, u64 b) { return a + b; });
+}
+
+// Where the border lies among the tokens of bucket b, of which `rank` tokens and `before`
+// weight lie above: the tokens of it from place sm.cut up are within, sm.w_cut is the
+// weight to there.  Returns how many tokens sm.list holds, the whole
+// bucket, or -1 if they were too many.
+template <bool BF16>
+__device__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, int b, u64 rank, u64 before,
+                        const Border &border)
+{
+    uint32_t lo = 0, hi = 0xFFFFFFFFu;
+    for (bool whole = true;; whole = false) {
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sm.n = 0;
+            sm.lo = 0xFFFFFFFFu;
+            sm.hi = 0;
+        }
+        __syncthreads();
+        uint32_t least = 0xFFFFFFFFu, most = 0;
+        row.template each<4>(0, row.chunks, [&](int c, const u32x4 &x) {
+#pragma unroll
+            for (int e = 0; e < Row<BF16>::EPC; ++e) {
+                const float v = Row<BF16>::get(x, e);
+                const uint32_t key = order_key(v);
+                if (weigh.bucket(v) == b && key >= lo && key <= hi) {
+                    const uint32_t i = atomicAdd(&sm.n, 1u);
+                    if (i < LIST)
+                        sm.list[i].place = place_of(v, row.index(c, e));
+                    least = min(least, key);
+                    most = max(most, key);
+                }
+            }
+        });
+        if (least <= most) {
+            atomicMin(&sm.lo, least);
+            atomicMax(&sm.hi, most);
+        }
+        __syncthreads();
+        const uint32_t n = sm.n;
+        lo = sm.lo;
+        hi = sm.hi;
+        const u64 none = ((u64)hi + 1) << 32;    // a cut above all of these (not above what was above them)
+        if (n <= LIST) {
+            const Compared t = compare_list(sm, (int)n, weigh);
+            const bool in = t.own && border.in(rank + t.rank, before + t.before, weigh.exact(logit_of(t.place)));
+            const u64 upto = before + block_sum(in ? t.w : 0, sm);
+            const u64 cut = block_all(in ? t.place : none, sm.scan, [](u64 x, u64 y) { return x < y ? x : y; });
+            if (threadIdx.x == 0) {
+                sm.cut = cut;
+                sm.w_cut = upto;
+            }
+            __syncthreads();
+            return whole ? (int)n : -1;
+        }
+        if (lo == hi) {
+            // ties: the first so many by index.  A thread takes chunks that follow one
+            // another
+            const float x = logit_of((u64)lo << 32);
+            const double own = weigh.exact(x);
+            const u64 w = weigh.weight(x);
+            u64 in = 0;
+            {   // the first token out, by halving
+                u64 out = n;
+                while (in < out) {
+                    const u64 mid = (in + out) / 2;
+                    if (border.in(rank + mid, before + mid * w, own))
+                        in = mid + 1;
+                    else
+                        out = mid;
+                }
+            }
+            const int per = (row.chunks + NT - 1) / NT;
+            const int c0 = min(row.chunks, (int)threadIdx.x * per), c1 = min(row.chunks, c0 + per);
+            u64 mine = 0, all;
+            for (int c = c0; c < c1; ++c) {
+                const u32x4 y = row.load(c);
+#pragma unroll
+                for (int e = 0; e < Row<BF16>::EPC; ++e)
+                    mine += order_key(Row<BF16>::get(y, e)) == lo;
+            }
+            u64 at = block_before(mine, sm.scan, all);
+            if (threadIdx.x == 0) {
+                sm.cut = none;
+                sm.w_cut = before + in * w;
+            }
+            __syncthreads();
+            if (in > at && in <= at + mine)
+                for (int c = c0; c < c1; ++c) {
+                    const u32x4 y = row.load(c);
+#pragma unroll
+                    for (int e = 0; e < Row<BF16>::EPC; ++e)
+                        if (order_key(Row<BF16>::get(y, e)) == lo && ++at == in)
+                            sm.cut = place_of(x, row.index(c, e));
+                }
+            __syncthreads();
+            return -1;
+        }
+        // too many: the part of the keys' range, from the top, in which the border lies
+        const uint32_t step = (hi - lo) / SUBS + 1;
+        for (int i = threadIdx.x; i < SUBS; i += NT) {
+            sm.w[i] = 0;
+            sm.w[SUBS + i] = 0;
+        }
+        if (threadIdx.x == 0)
+            sm.at = 0;
+        __syncthreads();
+        row.template each<2>(0, row.chunks, [&](int, const u32x4 &x) {
+#pragma unroll
+            for (int e = 0; e < Row<BF16>::EPC; ++e) {
+                const float v = Row<BF16>::get(x, e);
+                const uint32_t key = order_key(v);
+                if (weigh.bucket(v) == b && key >= lo && key <= hi) {
+                    atomicAdd(&sm.w[(hi - key) / step], weigh.weight(v));
+                    atomicAdd(&sm.w[SUBS + (hi - key) / step], 1ull);
+                }
+            }
+        });
+        __syncthreads();
+        u64 all;
+        const u64 wb = block_before(sm.w[threadIdx.x], sm.scan, all);
+        const u64 nb = block_before(sm.w[SUBS + threadIdx.x], sm.scan, all);
+        const uint32_t key = hi - threadIdx.x * step;    // the part's largest, if it is one
+        if (sm.w[SUBS + threadIdx.x] && border.in(rank + nb, before + wb, weigh.exact(logit_of((u64)key << 32))))
+            atomicMax(&sm.at, threadIdx.x);
+        __syncthreads();
+        if (threadIdx.x == sm.at) {
+            sm.slice[0] = wb;
+            sm.slice[1] = nb;
+        }
+        __syncthreads();
+        before += sm.slice[0];
+        rank += sm.slice[1];
+        const uint32_t part = sm.at;
+        const uint32_t below = hi - lo - part * step;   // keys of the range from the part's first down
+        hi = hi - part * step;
+        lo = below < step ? lo : hi - step + 1;
+    }
+}
+
+// `u` of a sum of weights, such that the token is the first whose sum is more
+__device__ __forceinline__ u64 goal_of(float u, u64 total)
+{
+    const double g = (double)u * (double)total;
+    const u64 t = g > 0.0 ? (u64)g : 0;
+    return t < total ? t : total - 1;
+}
+
+template <bool BF16, bool ONE>
+__device__ void choose_token(const SampleArgs &a, int b, Shared &sm, Slice one)
+{
+    const Row<BF16> row(a, b);
+    const Wish wish = wish_of(a, b);
+    const int S = ONE ? 1 : a.S;
+    float best = one.top;
+    bool few = one.n >= 0;
+    if (!ONE) {
+        best = -INFINITY;
+        few = true;
+        for (int s = 0; s < S; ++s) {
+            best = fmaxf(best, slice_at(a, b, s)->top);
+            few &= slice_at(a, b, s)->n >= 0;
+        }
+    }
+    double z = 0.0;
+    if (best > -INFINITY && best < INFINITY)
+        for (int s = 0; s < S; ++s) {
+            const Slice x = ONE ? one : *slice_at(a, b, s);
+            z += few && x.top > -INFINITY ? x.z * exp(((double)x.top - best) / wish.T) : x.z;
+        }
+    if (!(best > -INFINITY && best < INFINITY) || z != z) {
+        if (threadIdx.x == 0) {
+            a.token[b] = -1;
+            a.logp[b] = NAN;
+        }
+        return;
+    }
+    const float u = a.u[b];
+    const Weigher weigh = {best, 1.0 / (double)wish.T, sm.table};
+    if (!ONE || few)
+        fill_table(sm.table);
+    int token;
+    if (few) {
+        int n = one.n;
+        if (!ONE) {
+            n = 0;
+            for (int s = 0; s < S; ++s) {
+                const int ns = slice_at(a, b, s)->n;
+                for (int i = threadIdx.x; i < ns; i += NT)
+                    sm.list[n + i].place = a.lists[((size_t)b * S + s) * (LIST / S) + i];
+                n += ns;
+            }
+        }
+        __syncthreads();
+        const Compared t = compare_list(sm, n, weigh);
+        const u64 total = block_sum(t.own && t.rank < (u64)wish.k ? t.w : 0, sm);
+        const Border border = {(u64)wish.k, wish.p * (double)total, wish.min_p * UNIT};
+        const bool in = t.own && border.in(t.rank, t.before, weigh.exact(logit_of(t.place)));
+        const u64 kept = block_sum(in ? t.w : 0, sm), goal = goal_of(u, kept);
+        // the kept tokens' weights by index: again each with each
+        const int p = threads_each(n), i = threadIdx.x / p;
+        if (t.own)
+            sm.list[i].w = in ? t.w : 0;
+        __syncthreads();
+        if (i < n) {
+            u64 at = 0;
+            for (int j = threadIdx.x & (p - 1); j < n; j += p)
+                at += index_of(sm.list[j].place) < index_of(t.place) ? sm.list[j].w : 0;
+            for (int m = 1; m < p; m *= 2)
+                at += __shfl_xor(at, m);
+            if (in && at <= goal && goal < at + t.w)
+                sm.found = index_of(t.place);
+        }
+        __syncthreads();
+        token = sm.found;
+    } else {
+        if (!ONE)
+            for (int i = threadIdx.x; i < NB; i += NT) {
+                u64 w = 0;
+                uint32_t n = 0;
+                for (int s = 0; s < S; ++s) {
+                    w += a.weights[((size_t)b * S + s) * NB + i];
+                    n += a.counts[((size_t)b * S + s) * NB + i];
+                }
+                sm.hist[i] = w;
+                sm.count[i] = n;
+            }
+        __syncthreads();
+        // two buckets a thread: what lies before them
+        const int i0 = 2 * threadIdx.x;
+        u64 all, total;
+        const u64 n0 = block_before((u64)sm.count[i0] + sm.count[i0 + 1], sm.scan, all), n1 = n0 + sm.count[i0];
+        const u64 w0 = block_before(sm.hist[i0] + sm.hist[i0 + 1], sm.scan, total), w1 = w0 + sm.hist[i0];
+        z = (double)total / UNIT;
+        // the last bucket that holds a token within the border (the first does), and what
+        // is before it: in sm.at, sm.slice[0] and sm.slice[1]
+        auto last_bucket = [&](const Border &border) {
+            __syncthreads();
+            if (threadIdx.x == 0)
+                sm.at = 0;
+            __syncthreads();
+            // (a bucket's own weight: that of its lower end, the largest)
+            if (border.in(n0, w0, sm.table[i0]))
+                atomicMax(&sm.at, (uint32_t)i0);
+            if (border.in(n1, w1, sm.table[i0 + 1]))
+                atomicMax(&sm.at, (uint32_t)i0 + 1);
+            __syncthreads();
+            if (i0 == ((int)sm.at & ~1)) {
+                sm.slice[0] = sm.at & 1 ? n1 : n0;
+                sm.slice[1] = sm.at & 1 ? w1 : w0;
+            }
+            __syncthreads();
+        };
+        Border border = {(u64)1 << 62, INFINITY, 0.0};
+        u64 kept = total;            // by top-k
+        if (wish.k < a.V) {
+            border.k = wish.k;
+            last_bucket(border);
+            const int at = sm.at;
+            const u64 rank = sm.slice[0], before = sm.slice[1];
+            if (at < NB - 1) {
+                find_cut(row, sm, weigh, at, rank, before, border);
+                kept = sm.w_cut;
+            }
+        }
+        border.w = wish.p * (double)kept;
+        border.least = wish.min_p * UNIT;
+        last_bucket(border);
+        const int at = sm.at;
+        const u64 rank = sm.slice[0], before = sm.slice[1];
+        u64 cut = ~0ull;
+        kept = total;
+        int listed = 0;
+        if (at < NB - 1) {
+            listed = find_cut(row, sm, weigh, at, rank, before, border);
+            cut = sm.cut;
+            kept = sm.w_cut;
+        }
+        auto weight_in = [&](float x, int i) {
+            double r;
+            const int k = weigh.bucket(x, r);
+            return k < at || (k == at && k < NB - 1 && place_of(x, i) >= cut) ? weigh.rounded(k, r) : 0;
+        };
+        // the slice that the goal lies in, from the slices' sums
+        u64 goal = goal_of(u, kept);
+        int s = 0;
+        if (!ONE) {
+            __syncthreads();
+            if (threadIdx.x < MAX_SLICES)
+                sm.slice[threadIdx.x] = 0;
+            __syncthreads();
+            for (int i = threadIdx.x; i < S * NB; i += NT)
+                if (i % NB < at)
+                    atomicAdd(&sm.slice[i / NB], a.weights[((size_t)b * S + i / NB) * NB + i % NB]);
+            if (listed >= 0) {
+                for (int i = threadIdx.x; i < listed; i += NT)
+                    if (sm.list[i].place >= cut)
+                        atomicAdd(&sm.slice[even_part_of(row.chunks, S, (index_of(sm.list[i].place) + row.off) / Row<BF16>::EPC)],
+                                  sm.list[i].w);
+            } else
+                row.template each<2>(0, row.chunks, [&](int c, const u32x4 &x) {
+#pragma unroll
+                    for (int e = 0; e < Row<BF16>::EPC; ++e) {
+                        const float v = Row<BF16>::get(x, e);
+                        if (weigh.bucket(v) == at && place_of(v, row.index(c, e)) >= cut)
+                            atomicAdd(&sm.slice[even_part_of(row.chunks, S, c)], weigh.weight(v));
+                    }
+                });
+            __syncthreads();
+            while (s + 1 < S && goal >= sm.slice[s])
+                goal -= sm.slice[s++];
+        }
+        // and the token in it; a thread takes chunks that follow one another
+        const int begin = even_begin(row.chunks, S, s), end = even_begin(row.chunks, S, s + 1);
+        const int per = (end - begin + NT - 1) / NT;
+        const int c0 = min(end, begin + (int)threadIdx.x * per), c1 = min(end, c0 + per);
+        u64 mine = 0;
+        for (int c = c0; c < c1; ++c) {
+            const u32x4 x = row.load(c);
+#pragma unroll
+            for (int e = 0; e < Row<BF16>::EPC; ++e)
+                mine += weight_in(Row<BF16>::get(x, e), row.index(c, e));
+        }
+        u64 sum = block_before(mine, sm.scan, all);
+        if (threadIdx.x == 0)
+            sm.found = 0;
+        __syncthreads();
+        if (sum <= goal && goal < sum + mine)
+            for (int c = c0; c < c1; ++c) {
+                const u32x4 x = row.load(c);
+#pragma unroll
+                for (int e = 0; e < Row<BF16>::EPC; ++e) {
+                    const u64 w = weight_in(Row<BF16>::get(x, e), row.index(c, e));
+                    if (sum <= goal && goal < sum + w)
+                        sm.found = row.index(c, e);
+                    sum += w;
+                }
+            }
+        __syncthreads();
+        token = sm.found;
+    }
+    if (threadIdx.x == 0) {
+        a.token[b] = token;
+        a.logp[b] = (float)(((double)row.value(token) - best) / wish.T - log(z));
+    }
+}
+
+// ---- the kernels -------------------------------------------------------------------------
+
+template <bool BF16>
+__global__ __launch_bounds__(NT) void sample_one_kernel(SampleArgs a)
+{
+    __shared__ Shared sm;
+    const int b = blockIdx.x;
+    Slice one = find_candidates<BF16>(a, b, 0, sm);
+    __syncthreads();
+    if (one.n < 0 && one.top > -INFINITY && one.top < INFINITY)
+        one.z = fill_histogram<BF16>(a, b, 0, one.top, sm);
+    __syncthreads();
+    choose_token<BF16, true>(a, b, sm, one);
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(NT) void sample_candidates_kernel(SampleArgs a)
+{
+    __shared__ Shared sm;
+    const int b = blockIdx.x / a.S, s = blockIdx.x % a.S;
+    const Slice x = find_candidates<BF16>(a, b, s, sm);
+    for (int i = threadIdx.x; i < x.n; i += NT)
+        a.lists[((size_t)b * a.S + s) * (LIST / a.S) + i] = sm.list[i].place;
+    if (threadIdx.x == 0)
+        *slice_at(a, b, s) = x;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(NT) void sample_histogram_kernel(SampleArgs a)
+{
+    __shared__ Shared sm;
+    const int b = blockIdx.x / a.S, s = blockIdx.x % a.S;
+    float best = -INFINITY;
+    bool few = true;
+    for (int i = 0; i < a.S; ++i) {
+        best = fmaxf(best, slice_at(a, b, i)->top);
+        few &= slice_at(a, b, i)->n >= 0;
+    }
+    if (few || !(best > -INFINITY && best < INFINITY))
+        return;
+    const double z = fill_histogram<BF16>(a, b, s, best, sm);
+    for (int i = threadIdx.x; i < NB; i += NT) {
+        a.weights[((size_t)b * a.S + s) * NB + i] = sm.hist[i];
+        a.counts[((size_t)b * a.S + s) * NB + i] = sm.count[i];
+    }
+    if (threadIdx.x == 0)
+        slice_at(a, b, s)->z = z;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(NT) void sample_choose_kernel(SampleArgs a)
+{
+    __shared__ Shared sm;
+    choose_token<BF16, false>(a, blockIdx.x, sm, Slice{});
+}
+
+// Slices of a row: one workgroup takes rows of up to 32768 logits, and any where there
+// are rows for half of the CUs
+int slices_of(int B, int V)
+{
+    if (V <= 32768 || B >= 128)
+        return 1;
+    return std::max(1, std::min(std::min(512 / B, V / 8192), MAX_SLICES));
+}
+
+struct Workspace {
+    size_t slices, lists, weights, counts, all;
+};
+
+Workspace workspace_of(int B, int V)
+{
+    const size_t n = (size_t)B * slices_of(B, V);
+    Workspace w = {};
+    if (slices_of(B, V) == 1)
+        return w;
+    w.lists = w.slices + (n * sizeof(Slice) + 15) / 16 * 16;
+    w.weights = w.lists + (size_t)B * LIST * 8;
+    w.counts = w.weights + n * NB * 8;
+    w.all = w.counts + n * NB * 4;
+    return w;
+}
+
+ta_status check_sample_sizes(int B, int V)
+{
+    return B < 1 || V < 1 || B > MAX_B || V > MAX_V ? TA_ERR_INVALID_SHAPE : TA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const float *u, const float *temperature,
+                        const int *top_k, const float *top_p, const float *min_p, int *token, float *logp, int B,
+                        int V, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!logits || !u || !token || !logp)
+        return TA_ERR_NULL_POINTER;
+    const ta_status rc = check_sample_sizes(B, V);
+    if (rc != TA_OK)
+        return rc;
+    if (stride < 0 || stride > 1ll << 30)
+        return TA_ERR_INVALID_SHAPE;
+    if (misaligned(logits, l_bf16 ? 2 : 4) || misaligned(u, 4) || misaligned(temperature, 4) || misaligned(top_k, 4) ||
+        misaligned(top_p, 4) || misaligned(min_p, 4) || misaligned(token, 4) || misaligned(logp, 4))
+        return TA_ERR_MISALIGNED;
+    const size_t row = (size_t)B * 4;
+    const Span out[] = {{token, row}, {logp, row}};
+    const Span in[] = {{logits, (size_t)((B - 1) * stride + V) * (l_bf16 ? 2 : 4)}, {u, row}, {temperature, row},
+                       {top_k, row}, {top_p, row}, {min_p, row}};
+    if (overlaps(out[0], out[1]))
+        return TA_ERR_ALIASING;
+    for (const Span &s : in)
+        if (overlaps(out[0], s) || overlaps(out[1], s))
+            return TA_ERR_ALIASING;
+    const Workspace w = workspace_of(B, V);
+    if (w.all) {
+        if (!workspace || workspace_bytes < w.all)
+            return TA_ERR_WORKSPACE;
+        if (misaligned(workspace))
+            return TA_ERR_MISALIGNED;
+        const Span ws = {workspace, w.all};
+        if (overlaps(ws, out[0]) || overlaps(ws, out[1]))
+            return TA_ERR_ALIASING;
+        for (const Span &s : in)
+            if (overlaps(ws, s))
+                return TA_ERR_ALIASING;
+    }
+    unsigned char *const ws = (unsigned char *)workspace;
+    const SampleArgs a = {logits, stride, u, temperature, top_k, top_p, min_p, token, logp, V, slices_of(B, V),
+                          (Slice *)(ws + w.slices), (u64 *)(ws + w.lists), (u64 *)(ws + w.weights),
+                          (uint32_t *)(ws + w.counts)};
+    hipStream_t s = (hipStream_t)stream;
+    if (a.S == 1) {
+        hipLaunchKernelGGL(l_bf16 ? sample_one_kernel<true> : sample_one_kernel<false>, dim3(B), dim3(NT), 0, s, a);
+        return hipGetLastError() == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+    }
+    hipLaunchKernelGGL(l_bf16 ? sample_candidates_kernel<true> : sample_candidates_kernel<false>, dim3(B * a.S), dim3(NT), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(l_bf16 ? sample_histogram_kernel<true> : sample_histogram_kernel<false>, dim3(B * a.S), dim3(NT), 0, s, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) {
+        hipLaunchKernelGGL(l_bf16 ? sample_choose_kernel<true> : sample_choose_kernel<false>, dim3(B), dim3(NT), 0, s, a);
+        e = hipGetLastError();
+    }
+    return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
+}
+
+ta_status sample_workspace_bytes(int B, int V, size_t *bytes)
+{
+    if (!bytes)
+        return TA_ERR_NULL_POINTER;
+    const ta_status rc = check_sample_sizes(B, V);
+    if (rc != TA_OK)
+        return rc;
+    *bytes = workspace_of(B, V).all;
+    return TA_OK;
+}
+
+}  // extern "C"

@@ -134,6 +134,10 @@ def lib():
     L.gemm_mxfp4_workspace_bytes.argtypes = [i, i, i, i, ctypes.POINTER(ctypes.c_size_t)]
     L.gemm_mxfp4_plan.restype = i
     L.gemm_mxfp4_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
+    L.sample_logits.restype = i
+    L.sample_logits.argtypes = [p, ctypes.c_int64, i] + [p] * 7 + [i, i, p, ctypes.c_size_t, p]
+    L.sample_workspace_bytes.restype = i
+    L.sample_workspace_bytes.argtypes = [i, i, ctypes.POINTER(ctypes.c_size_t)]
     L.ta_schedule.restype = i
     L.ta_schedule.argtypes = [i, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
     L.ta_tile_shape.restype = i
@@ -1095,3 +1099,54 @@ def gemm_mxfp4_epilogue(a, w, w_scale, bias=None, activation: str = "none", resi
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return out
+
+
+@functools.lru_cache(maxsize=4096)
+def sample_workspace_bytes(B: int, V: int) -> int:
+    n = ctypes.c_size_t()
+    rc = lib().sample_workspace_bytes(B, V, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
+def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, token=None, logp=None,
+                  workspace=None, stream=None):
+    """(token [B] int32, logp [B] fp32): the next token of each row of logits [B, V] (fp32
+    or bf16; rows contiguous, of any stride) and the logarithm of its probability before
+    the filters.  u [B] are uniform numbers in [0, 1); temperature, top_p, min_p (fp32) and
+    top_k (int32) are GPU tensors [B], one number a row, or None: without.  A temperature
+    of 0 takes the largest logit, the first of several; a top_k of 0 does not limit.  Of the
+    tokens in falling order (equal ones by index) the first top_k stay, of these the
+    fewest that hold top_p of their weight, and those of min_p times the largest weight or
+    more; u picks one by the stayed weights' sums in the order of indexes.  A row without a
+    finite largest logit, or with NaN in it, gets token -1 and logp NaN.  ``workspace``, a
+    uint8 GPU tensor of at least sample_workspace_bytes(B, V) bytes, is allocated here if
+    needed and not given."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda:
+        raise TypeError("logits must be a 2-D float32 or bfloat16 GPU tensor [B, V]")
+    B, V = logits.shape
+    stride, step = logits.stride()
+    if V > 1 and step != 1:
+        raise TypeError("logits: each row must be contiguous")
+    _vector("u", u, torch.float32, (B,))
+    for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if t is not None:
+            _vector(name, t, dtype, (B,))
+    token = _output("token", token, (B,), torch.int32, logits)
+    logp = _output("logp", logp, (B,), torch.float32, logits)
+    need = sample_workspace_bytes(B, V)
+    if workspace is None:
+        if need:
+            workspace = _workspace(need, logits, stream)
+    elif workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous uint8 GPU tensor")
+    with _one_device(logits, u, temperature, top_k, top_p, min_p, token, logp, workspace):
+        rc = lib().sample_logits(logits.data_ptr(), stride if B > 1 else V, int(logits.dtype == torch.bfloat16),
+                                 u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                                 token.data_ptr(), logp.data_ptr(), B, V, _ptr(workspace),
+                                 workspace.numel() if workspace is not None else 0, _stream_handle(stream, logits))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return token, logp

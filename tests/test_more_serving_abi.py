@@ -108,6 +108,37 @@ def test_gemm_plan():
             ta.gemm_mxfp4_workspace_bytes(1, 8, 32, splits)
 
 
+L, U, TEMP, TOPK, TOPP, MINP, TOKEN, LOGP = (0x100000000 * i for i in range(1, 9))
+SAMPLE = dict(L=L, stride=50000, bf16=1, u=U, T=TEMP, k=TOPK, p=TOPP, m=MINP, token=TOKEN, logp=LOGP, B=3, V=50000, ws=WS,
+              ws_bytes=1 << 24, stream=None)
+SAMPLE_WS = ta.sample_workspace_bytes(3, 50000)
+
+
+@no_gpu
+@pytest.mark.parametrize("change,status", [
+    (dict(L=0), 1), (dict(u=0), 1), (dict(token=0), 1), (dict(logp=0), 1),
+    (dict(B=0), 2), (dict(V=0), 2), (dict(B=(1 << 16) + 1), 2), (dict(V=(1 << 20) + 1), 2), (dict(V=-1), 2),
+    (dict(stride=-1), 2), (dict(stride=(1 << 30) + 1), 2), (dict(stride=-50000), 2),
+    (dict(L=L + 1), 4), (dict(L=L + 2, bf16=0), 4), (dict(u=U + 2), 4), (dict(T=TEMP + 1), 4), (dict(k=TOPK + 2), 4),
+    (dict(p=TOPP + 2), 4), (dict(m=MINP + 3), 4), (dict(token=TOKEN + 2), 4), (dict(logp=LOGP + 1), 4),
+    (dict(token=LOGP + 4), 6), (dict(token=L), 6), (dict(logp=L + 2 * 149996), 6), (dict(logp=U), 6), (dict(token=TEMP), 6),
+    (dict(logp=TOPK - 4), 6), (dict(token=TOPP + 8), 6), (dict(logp=MINP), 6),
+    (dict(ws=0), 8), (dict(ws_bytes=SAMPLE_WS - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=L - 16), 6), (dict(ws=TOKEN), 6),
+    (dict(ws=LOGP - 1024), 6), (dict(ws=U - 64), 6), (dict(ws=TOPK), 6),
+], ids=str)
+def test_sample_refusals(change, status):
+    a = dict(SAMPLE, **change)
+    rc = ta.lib().sample_logits(*a.values())
+    assert rc == status, f"{change}: got {ta.STATUS.get(rc, rc)}, want {ta.STATUS[status]}"
+
+
+def test_sample_workspace():
+    assert ta.sample_workspace_bytes(1, 1) == 0 and 0 < SAMPLE_WS < 1 << 20
+    for bad in [(0, 10), (10, 0), ((1 << 16) + 1, 10), (10, (1 << 20) + 1)]:
+        with pytest.raises(ta.TileAttnError):
+            ta.sample_workspace_bytes(*bad)
+
+
 torch = pytest.importorskip("torch")
 BF16, U8, I32 = torch.bfloat16, torch.uint8, torch.int32
 
@@ -163,3 +194,16 @@ def test_gemm_checks(gpu_like, change):  # noqa: F811
     a = dict(a=torch.zeros(4, 64, dtype=BF16), w=torch.zeros(24, 32, dtype=U8), w_scale=torch.zeros(24, 2, dtype=U8))
     with pytest.raises((TypeError, ta.TileAttnError)):
         ta.gemm_mxfp4_epilogue(**dict(a, **change))
+
+
+@pytest.mark.parametrize("change", [
+    dict(logits=torch.zeros(3, 40, dtype=torch.float16)), dict(logits=torch.zeros(40)), dict(logits=torch.zeros(40, 3).t()),
+    dict(logits=torch.zeros(3, 80)[:, ::2]), dict(u=torch.zeros(2)), dict(u=torch.zeros(3, dtype=torch.float64)),
+    dict(temperature=torch.zeros(1)), dict(top_k=torch.zeros(3)), dict(top_k=torch.zeros(3, dtype=torch.int64)),
+    dict(top_p=torch.zeros(3, 1)), dict(min_p=torch.zeros(6)[::2]), dict(token=torch.zeros(3)),
+    dict(logp=torch.zeros(3, dtype=BF16)), dict(workspace=torch.zeros(100)),
+], ids=describe)
+def test_sample_checks(gpu_like, change):  # noqa: F811
+    a = dict(logits=torch.zeros(3, 40), u=torch.zeros(3))
+    with pytest.raises((TypeError, ta.TileAttnError)):
+        ta.sample_logits(**dict(a, **change))

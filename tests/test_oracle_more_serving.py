@@ -57,3 +57,21 @@ def test_norm_and_rotation():
         z = z * np.exp(1j * a[pos])[:, None]
         w = y[..., 0:32:2] + 1j * y[..., 1:32:2] if inter else y[..., :16] + 1j * y[..., 16:32]
         assert np.allclose(z, w)
+
+
+def test_sample():
+    x = np.log([4.0, 1.0, 2.0, 1.0])
+    one = lambda *a, **k: ms.sample(*a, **k)[0]    # noqa: E731
+    for u, t in ((0.0, 0), (0.49, 0), (0.51, 1), (0.63, 2), (0.9, 3)):
+        assert one(x, u) == [t] == one(x, u, error=1e-3)
+    assert np.isclose(ms.sample(x, 0.7)[1][0], np.log(0.25))
+    assert one(x, 0.9, top_k=3) == [2] and one(x, 0.6, top_k=3) == [1]      # order 0, 2, 1, 3
+    assert one(x, 0.99, top_p=0.5) == [0] and one(x, 0.99, top_p=0.51) == [2]
+    assert one(x, 0.99, top_p=0.499, error=0.01) == [0, 2] and one(x, 0.501, error=0.01) == [0, 1]
+    assert one(x, 0.99, min_p=0.3) == [2] and one(x, 0.99, min_p=0.6) == [0]
+    assert one(x, 0.99, top_p=0.0) == [0] and one(x, 0.99, min_p=2.0) == [0] and one(x, 0.99, min_p=np.nan) == [0]
+    assert one([1.0, 3.0, 3.0], 0.9, 0.0) == [1] and one(x, 0.9, top_p=np.nan) == [0]
+    assert one(x, 0.7, temperature=0.5) == [0] and one(x, 0.8, temperature=0.5) == [2]   # 16, 1, 4, 1
+    assert one([-np.inf, 0.0, -np.inf], 0.99) == [1]
+    for bad in ([np.nan, 1.0], [np.inf, 0.0], [-np.inf, -np.inf]):
+        assert one(bad, 0.5) == [-1]
