@@ -659,12 +659,14 @@ ta_status gemm_epilogue_route(int M, int N, int K, int num_splits, int *large_co
  *   N % 8 == 0 and K % 32 == 0 (else TA_ERR_UNSUPPORTED); sizes up to those of
  *   gemm_bf16_epilogue; A, W, bias, residual, C and workspace 16-byte aligned; C apart
  *   from A, W, W_scale and bias, and from residual unless it is C
- *   num_splits  1..64 (else TA_ERR_INVALID_SHAPE): ranges of K that separate workgroups
- *               sum, in whole steps of 128 (up to 64 rows: at most one for every eight
- *               steps); for more than one, each range's fp32 product goes to
- *               `workspace` (device, at least gemm_mxfp4_workspace_bytes(...) bytes, owned
- *               by the caller, no overlap with any other argument; TA_ERR_WORKSPACE if
- *               NULL or smaller) and a second kernel adds them in range order
+ *   num_parts  0..4096 (else TA_ERR_INVALID_SHAPE): the steps of K, 128 columns each, of
+ *               all strips (up to 64 rows) or tiles (more) of C are divided evenly over
+ *               this many workgroups, fewer where there are not as many steps (eight for
+ *               each, in strips); a second kernel adds what the division cuts, in order
+ *               of K, through `workspace` (device, at least
+ *               gemm_mxfp4_workspace_bytes(...) bytes, owned by the caller, no overlap with
+ *               any other argument; TA_ERR_WORKSPACE if NULL or smaller).  0: one
+ *               workgroup per strip or tile, no workspace
  *
  * The weights enter the products as the numbers that they stand for, exactly (those past
  * the largest bf16 number as infinity); a scale of 255 makes its row's column of C NaN.
@@ -673,14 +675,14 @@ ta_status gemm_epilogue_route(int M, int N, int K, int num_splits, int *large_co
  */
 ta_status gemm_mxfp4_epilogue(const void *A, const void *W, const void *W_scale, const void *bias,
                               const void *residual, void *C, int c_bf16, int activation, int M,
-                              int N, int K, int num_splits, void *workspace,
+                              int N, int K, int num_parts, void *workspace,
                               size_t workspace_bytes, void *stream);
 
-/* Workspace bytes gemm_mxfp4_epilogue needs, 0 for one range.  No HIP call. */
-ta_status gemm_mxfp4_workspace_bytes(int M, int N, int K, int num_splits, size_t *bytes);
+/* Workspace bytes gemm_mxfp4_epilogue needs for num_parts (0 for none).  No HIP call. */
+ta_status gemm_mxfp4_workspace_bytes(int M, int N, int K, int num_parts, size_t *bytes);
 
-/* A split count for gemm_mxfp4_epilogue.  No HIP call. */
-ta_status gemm_mxfp4_plan(int M, int N, int K, int *num_splits);
+/* A part count for gemm_mxfp4_epilogue.  No HIP call. */
+ta_status gemm_mxfp4_plan(int M, int N, int K, int *num_parts);
 
 /*
  * sample_logits — the next token of each row of logits, by temperature, top-k, top-p and

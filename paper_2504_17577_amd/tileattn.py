@@ -1028,9 +1028,9 @@ def gemm_bf16_epilogue(a, b, bias=None, activation: str = "none", residual=None,
     return out
 
 
-def gemm_mxfp4_workspace_bytes(M: int, N: int, K: int, num_splits: int) -> int:
+def gemm_mxfp4_workspace_bytes(M: int, N: int, K: int, num_parts: int) -> int:
     n = ctypes.c_size_t()
-    rc = lib().gemm_mxfp4_workspace_bytes(M, N, K, num_splits, ctypes.byref(n))
+    rc = lib().gemm_mxfp4_workspace_bytes(M, N, K, num_parts, ctypes.byref(n))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return n.value
@@ -1051,13 +1051,15 @@ def _mxfp4_launch(M, N, K):
 
 
 def gemm_mxfp4_epilogue(a, w, w_scale, bias=None, activation: str = "none", residual=None, out=None,
-                        out_dtype=None, stream=None, num_splits: int | None = None):
+                        out_dtype=None, stream=None, num_parts: int | None = None):
     """C = act(A W^T + bias) + residual for a contiguous bfloat16 GPU matrix a [M, K] (any
     M) and weights in 4 bits (MXFP4: e2m1 codes w [N, K / 2], uint8, the first of two in
     the low half, with a power of two for every 32 of a row, w_scale [N, K / 32], uint8;
     N a multiple of 8, K of 32), bias [N] bf16; C and residual [M, N] are float32
-    (default) or bfloat16 (``out_dtype``).  ``activation``, ``out`` and ``num_splits``
-    (default gemm_mxfp4_plan) as gemm_bf16_epilogue takes them."""
+    (default) or bfloat16 (``out_dtype``).  ``activation`` and ``out`` as
+    gemm_bf16_epilogue takes them.  The product's steps are divided over ``num_parts``
+    workgroups (default gemm_mxfp4_plan), through a workspace allocated here; 0, one per
+    strip or tile of C, needs none, and is the default where there is no memory for it."""
     if a.dtype != torch.bfloat16 or not a.is_cuda or a.dim() != 2 or not a.is_contiguous():
         raise TypeError("a must be a contiguous 2-D bfloat16 GPU tensor")
     M, K = a.shape
@@ -1080,22 +1082,22 @@ def gemm_mxfp4_epilogue(a, w, w_scale, bias=None, activation: str = "none", resi
     if residual is not None:
         _vector("residual", residual, dt, (M, N))
     out = _output("out", out, (M, N), dt, a)
-    chosen, ws = num_splits is None, None
+    chosen, ws = num_parts is None, None
     if chosen:
-        num_splits, need = _mxfp4_launch(M, N, K)
+        num_parts, need = _mxfp4_launch(M, N, K)
     else:
-        need = gemm_mxfp4_workspace_bytes(M, N, K, num_splits)
+        need = gemm_mxfp4_workspace_bytes(M, N, K, num_parts)
     if need:
         try:
             ws = _workspace(need, a, stream)
         except torch.OutOfMemoryError:
             if not chosen:
                 raise
-            num_splits, need = 1, 0   # the caller asked for no workspace: one range needs none
+            num_parts, need = 0, 0   # the caller asked for no workspace: whole strips and tiles need none
     with _one_device(a, w, w_scale, bias, residual, out):
         rc = lib().gemm_mxfp4_epilogue(a.data_ptr(), w.data_ptr(), w_scale.data_ptr(), _ptr(bias), _ptr(residual),
                                        out.data_ptr(), int(dt == torch.bfloat16), ACTIVATIONS[activation], M, N, K,
-                                       num_splits, _ptr(ws), need, _stream_handle(stream, a))
+                                       num_parts, _ptr(ws), need, _stream_handle(stream, a))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return out

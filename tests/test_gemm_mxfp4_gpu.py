@@ -58,12 +58,12 @@ def test_against_oracle(ta, M, N, K):
         c, tol = serving.gemm_epilogue(f64(a), v.T, f64(bias) if has_bias else None, act, f64(r) if has_res else None)
         if dt == BF16:
             tol = tol + 2.0 ** -8 * np.abs(c)
-        for splits in (None, 1, 2, 7):
+        for parts in (None, 0, 1, 3, 37, 256):
             got = ta.gemm_mxfp4_epilogue(a, w, s, bias=bias if has_bias else None, activation=act, residual=r, out_dtype=dt,
-                                         num_splits=splits)
+                                         num_parts=parts)
             assert got.dtype == dt and got.shape == (M, N)
             err = np.abs(f64(got) - c)
-            print(f"  {act} {has_bias} {has_res} {dt} splits {splits}: of bound {(err / tol).max():.2f}", flush=True)
+            print(f"  {act} {has_bias} {has_res} {dt} parts {parts}: of bound {(err / tol).max():.2f}", flush=True)
             assert (err <= tol).all()
 
 
@@ -76,8 +76,8 @@ def test_every_weight_counts_once(ta, M, N, K):
     w = torch.randint(0, 256, (N, K // 2), generator=g, dtype=U8)
     s = torch.randint(128, 131, (N, K // 32), generator=g, dtype=U8)
     want = f64(a) @ ms.mx_values(w.numpy(), s.numpy()).T
-    for splits in (None, 1, 3):
-        got = ta.gemm_mxfp4_epilogue(a, w.cuda(), s.cuda(), num_splits=splits)
+    for parts in (None, 1, 3):
+        got = ta.gemm_mxfp4_epilogue(a, w.cuda(), s.cuda(), num_parts=parts)
         np.testing.assert_array_equal(f64(got), want)
 
 
@@ -104,10 +104,10 @@ def test_onto_the_residual_in_place(ta, M, dt):
     g = torch.Generator().manual_seed(M)
     a, (w, s, _) = torch.randn(M, 1056, generator=g).to(BF16).cuda(), weights(264, 1056, g)
     x = torch.randn(M, 264, generator=g).to(dt).cuda()
-    for splits in (1, 3):
+    for parts in (1, 3):
         y = x.clone()
-        want = ta.gemm_mxfp4_epilogue(a, w, s, residual=x, out_dtype=dt, num_splits=splits)
-        assert ta.gemm_mxfp4_epilogue(a, w, s, residual=y, out=y, out_dtype=dt, num_splits=splits) is y
+        want = ta.gemm_mxfp4_epilogue(a, w, s, residual=x, out_dtype=dt, num_parts=parts)
+        assert ta.gemm_mxfp4_epilogue(a, w, s, residual=y, out=y, out_dtype=dt, num_parts=parts) is y
         assert torch.equal(y, want)
 
 
@@ -145,8 +145,8 @@ def test_guarded_rows(ta, M):
     a2.copy_(a), w2.copy_(w), s2.copy_(s)
     out = torch.full((M * N + 4096,), 5.0, device="cuda")
     c = out[2048:2048 + M * N].view(M, N)
-    for splits in (1, 2):
-        ta.gemm_mxfp4_epilogue(a2, w2, s2, out=c, num_splits=splits)
+    for parts in (1, 2):
+        ta.gemm_mxfp4_epilogue(a2, w2, s2, out=c, num_parts=parts)
         want, tol = serving.gemm_epilogue(f64(a), v.T)
         assert (np.abs(f64(c) - want) <= tol).all()
         assert (out[:2048] == 5).all() and (out[2048 + M * N:] == 5).all()

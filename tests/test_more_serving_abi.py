@@ -69,7 +69,7 @@ def test_attention_refusals(change, status):
 
 
 A, W, S, BIAS, R, C = (0x100000000 * i for i in range(1, 7))
-GEMM = dict(A=A, W=W, S=S, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=4128, splits=2, ws=WS,
+GEMM = dict(A=A, W=W, S=S, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=4128, parts=2, ws=WS,
             ws_bytes=1 << 20, stream=None)
 
 
@@ -78,11 +78,11 @@ GEMM = dict(A=A, W=W, S=S, bias=BIAS, R=R, C=C, c_bf16=0, act=1, M=40, N=64, K=4
     (dict(A=0), 1), (dict(W=0), 1), (dict(S=0), 1), (dict(C=0), 1),
     (dict(M=0), 2), (dict(N=0), 2), (dict(K=-32), 2), (dict(N=1 << 24), 2), (dict(K=1 << 22), 2),
     (dict(M=1 << 20, N=1 << 15), 2), (dict(M=1 << 20, K=1 << 20), 2), (dict(M=(1 << 20) + 1), 2), (dict(N=1 << 22, K=1 << 18), 2),
-    (dict(splits=0), 2), (dict(splits=65), 2), (dict(N=60), 3), (dict(K=4112), 3), (dict(act=-1), 3), (dict(act=5), 3),
+    (dict(parts=-1), 2), (dict(parts=4097), 2), (dict(N=60), 3), (dict(K=4112), 3), (dict(act=-1), 3), (dict(act=5), 3),
     (dict(A=A + 8), 4), (dict(W=W + 2), 4), (dict(C=C + 4), 4), (dict(bias=BIAS + 8), 4), (dict(R=R + 4), 4),
     (dict(C=A + 16), 6), (dict(C=W + 16), 6), (dict(C=S), 6), (dict(S=C + 64 * 40 * 4 - 1), 6), (dict(C=BIAS), 6),
     (dict(R=C + 16), 6), (dict(R=C - 16), 6),
-    (dict(ws=0), 8), (dict(ws_bytes=2 * 40 * 64 * 4 - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=A), 6), (dict(ws=W + 1024), 6),
+    (dict(ws=0), 8), (dict(ws_bytes=2 * 2 * 40 * 64 * 4 - 1), 8), (dict(ws=WS + 8), 4), (dict(ws=A), 6), (dict(ws=W + 1024), 6),
     (dict(ws=S + 16), 6), (dict(ws=C - 16), 6), (dict(ws=R), 6), (dict(ws=BIAS), 6),
 ], ids=str)
 def test_gemm_refusals(change, status):
@@ -96,16 +96,21 @@ def test_gemm_plan():
         for N in (8, 64, 1000, 4096, 65536):
             for K in (32, 64, 992, 4096, 65536):
                 n = ta.gemm_mxfp4_plan(M, N, K)
-                assert 1 <= n <= 64 and ta.gemm_mxfp4_workspace_bytes(M, N, K, 1) == 0
-                assert ta.gemm_mxfp4_workspace_bytes(M, N, K, 64) % (4 * M * N) == 0
+                assert 0 <= n <= 256 and ta.gemm_mxfp4_workspace_bytes(M, N, K, 0) == 0
+                assert (ta.gemm_mxfp4_workspace_bytes(M, N, K, n) > 0) == (n > 0)
+    assert ta.gemm_mxfp4_workspace_bytes(40, 64, 4128, 2) == 2 * 2 * 40 * 64 * 4        # two records of a strip each
+    assert ta.gemm_mxfp4_workspace_bytes(40, 64, 256, 30) == 2 * 2 * 40 * 64 * 4        # two steps
+    assert ta.gemm_mxfp4_workspace_bytes(3, 64, 4096, 30) == 16 * 2 * 3 * 16 * 4        # 128 steps, eight waves
+    assert ta.gemm_mxfp4_workspace_bytes(100, 256, 1024, 9) == 9 * 2 * 128 * 128 * 4    # tiles
+    assert ta.gemm_mxfp4_workspace_bytes(1 << 20, 1 << 14, 1 << 20, 9) == 0             # steps past 32 bits: whole tiles
     for bad in [(0, 8, 32), (1, 0, 32), (1, 8, -32), (1, 12, 32), (1, 8, 48), (1, 1 << 24, 32)]:
         with pytest.raises(ta.TileAttnError):
             ta.gemm_mxfp4_plan(*bad)
         with pytest.raises(ta.TileAttnError):
             ta.gemm_mxfp4_workspace_bytes(*bad, 2)
-    for splits in (0, 65):
+    for parts in (-1, 4097):
         with pytest.raises(ta.TileAttnError):
-            ta.gemm_mxfp4_workspace_bytes(1, 8, 32, splits)
+            ta.gemm_mxfp4_workspace_bytes(1, 8, 32, parts)
 
 
 L, U, TEMP, TOPK, TOPP, MINP, TOKEN, LOGP = (0x100000000 * i for i in range(1, 9))
