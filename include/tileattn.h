@@ -573,7 +573,7 @@ ta_status qk_norm_rope_append(const void *Q, const void *K, const void *V, int64
  *   K_cache, V_cache  device, codes, uint8 [num_pages, Hkv, page_size, D / 2]
  *   k_scale, v_scale  device, scales, uint8 [num_pages, Hkv, page_size, D / 32],
  *                     16-byte aligned, not NULL
- * Everything else as attn_decode_paged, with its plan and its workspace: keys and values
+ * Everything else as attn_decode_paged, with its workspace: keys and values
  * enter the products as the numbers they stand for, exactly (those past the largest bf16
  * number as infinity); a scale of 255 within a sequence's positions makes what it enters
  * NaN.
@@ -594,6 +594,10 @@ ta_status attn_paged_workspace_bytes(int Hq, int Hkv, int D, int num_parts, size
  * instead of 9.5, 32 of 200 9 instead of 14).  No HIP call. */
 ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages,
                           int *num_parts);
+
+/* The same for attn_decode_paged_mxfp4.  No HIP call. */
+ta_status attn_paged_mxfp4_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages,
+                                int *num_parts);
 
 /* Activations of gemm_bf16_epilogue */
 typedef enum {

@@ -5,6 +5,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cache_checks.h"
 #include "mxfp4.h"
 #include "paged_plan.h"
@@ -252,7 +254,8 @@ template <int D, int TYPE, int RT>
 __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
     constexpr bool E4M3 = TYPE == TA_CACHE_E4M3, MX = TYPE == TA_CACHE_MXFP4;
-    constexpr int KB = MX && RT == 1 ? 4 : 2;    // 16-key blocks per wave and step
+    constexpr int KB = 2;                        // 16-key blocks per wave and step
+    constexpr int AHEAD = 1;                     // steps that loads are ahead
     constexpr int KS = 16 * KB;
     constexpr int KK = D / 32;                   // k-steps of the scores
     constexpr int ROW = MX ? D / 2 : D * (E4M3 ? 1 : 2);   // bytes of a key
@@ -344,21 +347,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 page[kb] = table[min(((first + s * KS) >> 4) + kb, last_block) >> (a.page_shift - 4)];
         };
         size_t at[KB];             // (MXFP4: the rows before it)
-        bool bad[KB], next_bad[KB];
-        auto place = [&](int s) {
+        bool bad[KB], next_bad[AHEAD][KB];
+        auto place = [&](int s, int buf) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const int pg = paged_checked(page[kb], a.num_pages);
                 const int blk = min(((first + s * KS) >> 4) + kb, last_block);
                 const int in = (blk << 4) & ((1 << a.page_shift) - 1);
                 at[kb] = ((((size_t)max(pg, 0) * a.Hkv + h) << a.page_shift) + in) * (MX ? 1 : ROW);
-                next_bad[kb] = pg < 0;
+                next_bad[buf][kb] = pg < 0;
             }
         };
-        u32x4 kr[KB][KL];
-        uint32_t vr[KB][4][VW];
-        uint32_t kx[KB], vx[KB];   // MXFP4: a key's scales
-        auto load_k = [&]() {
+        u32x4 k_buf[AHEAD][KB][KL];
+        uint32_t v_buf[AHEAD][KB][4][VW];
+        uint32_t kx_buf[AHEAD][KB], vx_buf[AHEAD][KB];   // MXFP4: a key's scales
+        auto load_k = [&](int buf) {
+            auto &kr = k_buf[buf];
+            auto &kx = kx_buf[buf];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const unsigned char *p = (const unsigned char *)a.K + at[kb] * (MX ? ROW : 1);
@@ -381,7 +386,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 }
             }
         };
-        auto load_v = [&]() {
+        auto load_v = [&](int buf) {
+            auto &vr = v_buf[buf];
+            auto &vx = vx_buf[buf];
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const unsigned char *p = (const unsigned char *)a.V + at[kb] * (MX ? ROW : 1);
@@ -411,17 +418,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             }
         };
 
-        if (steps > 0) {
+        if (steps > 0)
             lookup(0);
-            place(0);
-            load_k();
-            load_v();
-            if (steps > 1)
-                lookup(1);
-        }
-        for (int s = 0; s < steps; ++s) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (i < steps) {
+                place(i, i);
+                load_k(i);
+                load_v(i);
+                if (i + 1 < steps)
+                    lookup(i + 1);
+            }
+        // `tail`: whether there are keys past the last in the step (uniform)
+        auto step = [&](int s, auto buf_of, auto tail) {
+            constexpr int buf = buf_of;
+            auto &kr = k_buf[buf];
+            auto &vr = v_buf[buf];
             const int key0 = first + s * KS;
-            const bool tail = key0 + KS > k_hi;      // uniform
             // The K loads took whole lines of eight rows each (halves of sixteen rows'
             // lines would come from HBM twice); lanes c16 and c16 ^ 8 exchange what the
             // other's row needs: then lane c16 holds chunks 8 l + g and 8 l + 4 + g of row c16
@@ -448,7 +461,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                     for (int kk = 0; kk < KK; ++kk) {
                         bf16x8 k;
                         if constexpr (MX) {
-                            k = tileattn_mx::eight(kr[kb][0][kk], tileattn_mx::scale_of(kx[kb]));
+                            k = tileattn_mx::eight(kr[kb][0][kk], tileattn_mx::scale_of(kx_buf[buf][kb]));
                         } else if constexpr (E4M3) {
                             const uint32_t w0 = kr[kb][kk >> 1][2 * (kk & 1)], w1 = kr[kb][kk >> 1][2 * (kk & 1) + 1];
                             k = __builtin_bit_cast(bf16x8, u32x4{e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
@@ -461,12 +474,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 }
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-                bad[kb] = next_bad[kb];
-            if (s + 1 < steps) {
-                place(s + 1);
-                load_k();
-                if (s + 2 < steps)
-                    lookup(s + 2);
+                bad[kb] = next_bad[buf][kb];
+            if (s + AHEAD < steps) {
+                place(s + AHEAD, buf);
+                load_k(buf);
+                if (s + AHEAD + 1 < steps)
+                    lookup(s + AHEAD + 1);
             }
             // a page outside the pool makes its keys' scores NaN, and so the row
 #pragma unroll
@@ -482,7 +495,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             if constexpr (MX) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
-                    const int x = (int)(((vx[kb] >> (8 * (c16 * XG / 16))) & 0xFF) << 23);
+                    const int x = (int)(((vx_buf[buf][kb] >> (8 * (c16 * XG / 16))) & 0xFF) << 23);
                     vsc[kb][0] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0x00, 0xF, 0xF, true));
                     vsc[kb][1] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0x55, 0xF, 0xF, true));
                     vsc[kb][2] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0xAA, 0xF, 0xF, true));
@@ -594,8 +607,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                         }
                 }
             }
-            if (s + 1 < steps)
-                load_v();
+            if (s + AHEAD < steps)
+                load_v(buf);
+        };
+        typedef std::integral_constant<int, 0> Even;
+        if constexpr (MX) {
+            // the last step by itself: the masks in every step, for the last one's sake, were a
+            // sixth of the vector instructions
+            for (int s = 0; s + 1 < steps; ++s)
+                step(s, Even{}, std::false_type{});
+            if (steps > 0)
+                step(steps - 1, Even{}, std::true_type{});
+        } else {
+            for (int s = 0; s < steps; ++s)
+                step(s, Even{}, first + (s + 1) * KS > k_hi);
         }
 
         // The waves' sums meet in LDS, in wave order.  Lane: row c16, dims
@@ -963,6 +988,18 @@ ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_
     const int64_t heads = (int64_t)B * Hkv * paged_row_blocks(Hq / Hkv);
     *num_parts = cap <= 768 || (cap <= 1024 && heads >= 1024) || heads >= 2 * cap ? 0 : 512;
     return TA_OK;
+}
+
+// The keys of a cache in 4 bits cost more of the vector ALU's time than of HBM's: three
+// workgroups on a CU hide each other's loads better than two.  us, 512 | 768 | 1024 parts:
+// 64 sequences mixed to 16384 44.0 | 40.4 | 43.3, one of 100001 32.2 | 31.6 | 35.1, 32 mixed to
+// 4000 with 32 K/V heads of 64 dims 29.6 | 25.7 | 25.3
+ta_status attn_paged_mxfp4_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages, int *num_parts)
+{
+    const ta_status rc = attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages, num_parts);
+    if (rc == TA_OK && *num_parts)
+        *num_parts = 768;
+    return rc;
 }
 
 }  // extern "C"

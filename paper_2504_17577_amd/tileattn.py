@@ -120,6 +120,8 @@ def lib():
     L.attn_paged_workspace_bytes.argtypes = [i] * 4 + [ctypes.POINTER(ctypes.c_size_t)]
     L.attn_paged_plan.restype = i
     L.attn_paged_plan.argtypes = [i] * 6 + [ctypes.POINTER(i)]
+    L.attn_paged_mxfp4_plan.restype = i
+    L.attn_paged_mxfp4_plan.argtypes = L.attn_paged_plan.argtypes
     L.gemm_bf16_epilogue.restype = i
     L.gemm_bf16_epilogue.argtypes = [p] * 5 + [i] * 6 + [p, ctypes.c_size_t, p]
     L.gemm_epilogue_workspace_bytes.restype = i
@@ -892,9 +894,18 @@ def attn_paged_plan(B: int, Hq: int, Hkv: int, D: int, page_size: int, max_pages
     return n.value
 
 
+def attn_paged_mxfp4_plan(B: int, Hq: int, Hkv: int, D: int, page_size: int, max_pages: int) -> int:
+    n = ctypes.c_int()
+    rc = lib().attn_paged_mxfp4_plan(B, Hq, Hkv, D, page_size, max_pages, ctypes.byref(n))
+    if rc != TA_OK:
+        raise TileAttnError(rc, ta_status_string(rc))
+    return n.value
+
+
 @functools.lru_cache(maxsize=4096)
-def _paged_launch(B, Hq, Hkv, D, page_size, max_pages):
-    n = attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages)
+def _paged_launch(B, Hq, Hkv, D, page_size, max_pages, kind=0):
+    plan = attn_paged_mxfp4_plan if kind == MXFP4 else attn_paged_plan
+    n = plan(B, Hq, Hkv, D, page_size, max_pages)
     return n, attn_paged_workspace_bytes(Hq, Hkv, D, n)
 
 
@@ -907,7 +918,8 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
     bits), table and scales as kv_cache_append takes them.  ``scale`` defaults to 1/sqrt(D),
     ``out_dtype`` is torch.float32 (default) or torch.bfloat16.  A sequence of
     length 0 gets O = 0 and LSE = -inf.  The batch's positions are divided over
-    ``num_parts`` workgroups (default attn_paged_plan, from the table's capacity; 0,
+    ``num_parts`` workgroups (default attn_paged_plan or, for 4 bits,
+    attn_paged_mxfp4_plan, from the table's capacity; 0,
     one a head, is faster for short sequences behind a large table); ``workspace``, a uint8 GPU
     tensor of at least attn_paged_workspace_bytes(...) bytes, is allocated here if
     needed and not given; it must stay alive until the launch has finished on
@@ -927,7 +939,7 @@ def attn_decode_paged(q, k_cache, v_cache, page_table, seq_lens, scale: float | 
     out = _output("out", out, (B, Hq, D), o_dtype, q)
     lse = _output("lse", lse, (B, Hq), torch.float32, q)
     if num_parts is None:
-        num_parts, need = _paged_launch(B, Hq, Hkv, D, page_size, max_pages)
+        num_parts, need = _paged_launch(B, Hq, Hkv, D, page_size, max_pages, kind)
     else:
         need = attn_paged_workspace_bytes(Hq, Hkv, D, num_parts)
     if workspace is None:

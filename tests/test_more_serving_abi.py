@@ -102,7 +102,7 @@ def test_gemm_plan():
     assert ta.gemm_mxfp4_workspace_bytes(40, 64, 256, 30) == 2 * 2 * 40 * 64 * 4        # two steps
     assert ta.gemm_mxfp4_workspace_bytes(3, 64, 4096, 30) == 16 * 2 * 3 * 16 * 4        # 128 steps, eight waves
     assert ta.gemm_mxfp4_workspace_bytes(100, 256, 1024, 9) == 9 * 2 * 128 * 128 * 4    # tiles
-    assert ta.gemm_mxfp4_workspace_bytes(1 << 20, 1 << 14, 1 << 20, 9) == 0             # steps past 32 bits: whole tiles
+    assert ta.gemm_mxfp4_workspace_bytes(1 << 20, 1 << 14, (1 << 20) - 32, 9) == 0             # steps past 32 bits: whole tiles
     for bad in [(0, 8, 32), (1, 0, 32), (1, 8, -32), (1, 12, 32), (1, 8, 48), (1, 1 << 24, 32)]:
         with pytest.raises(ta.TileAttnError):
             ta.gemm_mxfp4_plan(*bad)
