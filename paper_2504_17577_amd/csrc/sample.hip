@@ -7,14 +7,13 @@
 // computed in 64 bits and added as whole multiples of 2^-43: exactly, in any order.
 // What is less than half of that counts as nothing.
 //
-// Nothing is sorted.  A small top-k (this covers greedy rows) takes candidates:
-// the largest logits of a few thousand groups give a border that at least k tokens are
-// above and few more; those alone are weighed and compared, each with each.  Otherwise a histogram of the
-// weights over (best - x) / T, in 2047 buckets of 31 / 2048, finds the bucket in which
-// the place lies, and the tokens of that bucket alone are compared; should they be too
-// many (ties, most of all), their keys' range is narrowed in the same way.  The chosen
-// token is then found in the order of indexes, from the sums of slices of the row, in
-// one slice.
+// Nothing is sorted.  A small top-k (this covers greedy rows) takes candidates: the
+// largest logits of a few thousand groups give a border that at least k tokens are above
+// and few more; the place is found among those alone.  Otherwise a histogram of the
+// weights over (best - x) / T, in 2047 buckets of 31 / 2048, shows the bucket that the
+// place lies in, and it is found among the tokens of that bucket; should they be too many
+// (ties, most of all), their keys' range is narrowed in the same way.  The token is then
+// found in the order of indexes, from the sums of slices of the row, in one slice.
 //
 // A row is cut into slices for a few large rows: a kernel over slices for the largest
 // logit and the candidates, one over slices for the histograms (rows that need none
@@ -41,9 +40,11 @@ constexpr int NT = 1024, NWAVE = NT / 64;
 constexpr int NB = 2048;                 // buckets; the last holds what counts as nothing
 constexpr double BUCKET = 31.0 / NB, PER_UNIT = NB / 31.0;
 constexpr double UNIT = 0x1p43;
-constexpr int LIST = 1024;               // tokens that are compared with each other, at most one a thread
+constexpr int LIST = NT;                 // tokens that are looked at by themselves, one a thread
+constexpr int FEW = 128;                 // of which so many are compared with each other
 constexpr int CANDIDATES = 512;          // as many times the slices as a top-k may ask for to have candidates
 constexpr int GROUPS = 4;                // of a thread, whose largest logits set the border
+constexpr int HELD = 17;                 // chunks of 16 bytes of a slice that a thread holds (131072 16-bit logits and a piece)
 constexpr int SUBS = 1024;               // parts of a bucket's range of keys
 constexpr int MAX_SLICES = 32;
 constexpr int MAX_V = 1 << 20, MAX_B = 1 << 16;
@@ -74,68 +75,120 @@ struct __attribute__((aligned(16))) Token {
 };
 
 struct Shared {
-    Token list[LIST];
-    u64 w[2 * SUBS];
+    u64 list[LIST];          // places
+    Token few[LIST];
+    u64 w[SUBS];
+    uint32_t n_of[SUBS];
     double table[NB];        // weight of a bucket's lower end, in units
     u64 hist[NB];
     uint32_t count[NB];
-    u64 scan[NWAVE], slice[MAX_SLICES], w_cut;
+    u64 scan[NWAVE], sum[2][NWAVE], slice[MAX_SLICES], w_cut;
     double z[NWAVE];
     float best[NWAVE], low[NWAVE];
-    uint32_t n, lo, hi, at;
-    u64 cut;
+    uint32_t n, lo, hi, at, n_few;
+    u64 cut, low_place, high_place, rank, before;
     int found;
 };
 
 // ---- the workgroup's sums ---------------------------------------------------
 
-template <class F, class Op>
-__device__ __forceinline__ F wave_all(F x, Op op)
+// x moved by a lane pattern of the vector ALU; lanes that nothing moves to get `none`
+template <int CTRL, int ROWS, class F>
+__device__ __forceinline__ F moved(F x, F none)
 {
-#pragma unroll
-    for (int m = 32; m; m >>= 1)
-        x = op(x, __shfl_xor(x, m));
-    return x;
+    if constexpr (sizeof(F) == 4) {
+        return __builtin_bit_cast(F, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x),
+                                                                 CTRL, ROWS, 0xF, false));
+    } else {
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        const i32x2 v = __builtin_bit_cast(i32x2, x), n = __builtin_bit_cast(i32x2, none);
+        return __builtin_bit_cast(F, i32x2{__builtin_amdgcn_update_dpp(n[0], v[0], CTRL, ROWS, 0xF, false),
+                                           __builtin_amdgcn_update_dpp(n[1], v[1], CTRL, ROWS, 0xF, false)});
+    }
 }
 
-// op over all threads' x, through NWAVE places of LDS
+// op over the lanes up to this one: rows of sixteen by shifts, then the rows' last lanes
 template <class F, class Op>
-__device__ __forceinline__ F block_all(F x, F *s, Op op)
+__device__ __forceinline__ F wave_upto(F x, F none, Op op)
 {
-    x = wave_all(x, op);
-    __syncthreads();
+    x = op(x, moved<0x111, 0xF>(x, none));     // row_shr:1, 2, 4, 8
+    x = op(x, moved<0x112, 0xF>(x, none));
+    x = op(x, moved<0x114, 0xF>(x, none));
+    x = op(x, moved<0x118, 0xF>(x, none));
+    x = op(x, moved<0x142, 0xA>(x, none));     // row_bcast:15 to rows 1 and 3
+    return op(x, moved<0x143, 0xC>(x, none));  // row_bcast:31 to rows 2 and 3
+}
+
+// op over all lanes, the same in each
+template <class F, class Op>
+__device__ __forceinline__ F wave_all(F x, F none, Op op)
+{
+    x = wave_upto(x, none, op);
+    if constexpr (sizeof(F) == 4) {
+        return __builtin_bit_cast(F, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+    } else {
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        const i32x2 v = __builtin_bit_cast(i32x2, x);
+        return __builtin_bit_cast(F, i32x2{__builtin_amdgcn_readlane(v[0], 63), __builtin_amdgcn_readlane(v[1], 63)});
+    }
+}
+
+__device__ __forceinline__ u64 wave_sum_upto(u64 x) { return wave_upto(x, (u64)0, [](u64 a, u64 b) { return a + b; }); }
+
+template <class F>
+__device__ __forceinline__ F from_lane(F x, int lane)       // (lane: uniform)
+{
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 v = __builtin_bit_cast(i32x2, x);
+    return __builtin_bit_cast(F, i32x2{__builtin_amdgcn_readlane(v[0], lane), __builtin_amdgcn_readlane(v[1], lane)});
+}
+
+// op over all threads' x, through NWAVE places of LDS that nobody reads any more
+template <class F, class Op>
+__device__ __forceinline__ F block_all(F x, F none, F *s, Op op)
+{
+    x = wave_all(x, none, op);
     if (threadIdx.x % 64 == 0)
         s[threadIdx.x / 64] = x;
     __syncthreads();
-    x = s[0];
-#pragma unroll
-    for (int i = 1; i < NWAVE; ++i)
-        x = op(x, s[i]);
-    return x;
+    return wave_all(threadIdx.x % 64 < NWAVE ? s[threadIdx.x % 64] : none, none, op);
 }
 
-// The sum of the threads' x before this one; `all`: of all
+// The sum of the threads' x before this one; `all`: of all (s as above)
 __device__ __forceinline__ u64 block_before(u64 x, u64 *s, u64 &all)
 {
-    u64 in = x;
-    const int lane = threadIdx.x % 64;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 y = __shfl_up(in, d);
-        in += lane >= d ? y : 0;
-    }
-    __syncthreads();
-    if (lane == 63)
+    const u64 in = wave_sum_upto(x);
+    if (threadIdx.x % 64 == 63)
         s[threadIdx.x / 64] = in;
     __syncthreads();
-    u64 before = 0;
-    all = 0;
-#pragma unroll
-    for (int i = 0; i < NWAVE; ++i) {
-        before += i < (int)threadIdx.x / 64 ? s[i] : 0;
-        all += s[i];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const u64 upto = wave_sum_upto(threadIdx.x % 64 < NWAVE ? s[threadIdx.x % 64] : 0);
+    all = from_lane(upto, NWAVE - 1);
+    return (wave ? from_lane(upto, wave - 1) : 0) + in - x;
+}
+
+// Two such sums at once, in place
+__device__ __forceinline__ void block_before2(u64 &x, u64 &y, u64 (*s)[NWAVE], u64 &all_y)
+{
+    const u64 in_x = wave_sum_upto(x), in_y = wave_sum_upto(y);
+    if (threadIdx.x % 64 == 63) {
+        s[0][threadIdx.x / 64] = in_x;
+        s[1][threadIdx.x / 64] = in_y;
     }
-    return before + in - x;
+    __syncthreads();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const u64 upto_x = wave_sum_upto(lane < NWAVE ? s[0][lane] : 0), upto_y = wave_sum_upto(lane < NWAVE ? s[1][lane] : 0);
+    all_y = from_lane(upto_y, NWAVE - 1);
+    x = (wave ? from_lane(upto_x, wave - 1) : 0) + in_x - x;
+    y = (wave ? from_lane(upto_y, wave - 1) : 0) + in_y - y;
+}
+
+// *last = the largest n of the threads with `is` (n rises with the thread): one atomic a wave
+__device__ __forceinline__ void note_last(uint32_t *last, bool is, uint32_t n)
+{
+    const u64 mask = __builtin_amdgcn_ballot_w64(is);
+    if (mask && threadIdx.x % 64 == 63 - __builtin_clzll(mask))
+        atomicMax(last, n);
 }
 
 // ---- a row -------------------------------------------------------------------
@@ -168,10 +221,9 @@ struct Row {
     {
         if (c * EPC >= off && (c + 1) * EPC <= off + V)
             return *(const u32x4 *)(line + (size_t)16 * c);
-        u32x4 x;
+        u32x4 x = nothing();
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            x[w] = BF16 ? 0xFF80FF80u : 0xFF800000u;
             if (BF16) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -183,6 +235,11 @@ struct Row {
             }
         }
         return x;
+    }
+    static __device__ __forceinline__ u32x4 nothing()
+    {
+        const uint32_t w = BF16 ? 0xFF80FF80u : 0xFF800000u;    // -inf
+        return u32x4{w, w, w, w};
     }
     static __device__ __forceinline__ float get(const u32x4 &x, int e)
     {
@@ -212,7 +269,7 @@ struct Row {
 
 // What a row asks for
 struct Wish {
-    float T;
+    float T, u;
     int k;           // V: no limit
     bool few;        // candidates
     double p, min_p;
@@ -220,7 +277,7 @@ struct Wish {
 
 __device__ __forceinline__ Wish wish_of(const SampleArgs &a, int b)
 {
-    Wish w = {1.f, a.V, false, INFINITY, 0.0};
+    Wish w = {1.f, a.u[b], a.V, false, INFINITY, 0.0};
     if (a.top_k && a.top_k[b] > 0)
         w.k = min(a.top_k[b], a.V);
     if (a.top_p)
@@ -234,7 +291,7 @@ __device__ __forceinline__ Wish wish_of(const SampleArgs &a, int b)
         else
             w.k = 1;                 // greedy
     }
-    w.few = (int64_t)w.k * a.S <= CANDIDATES;
+    w.few = (int64_t)w.k * a.S <= CANDIDATES || (a.S == 1 && a.V <= LIST);
     return w;
 }
 
@@ -309,55 +366,95 @@ __device__ __forceinline__ Slice *slice_at(const SampleArgs &a, int b, int s) { 
 
 // ---- 1: a slice's largest logit and candidates ------------------------------------
 
+// A thread's chunks of a slice, every NT-th, in registers: the row is read once
 template <bool BF16>
-__device__ Slice find_candidates(const SampleArgs &a, int b, int s, Shared &sm)
-{
-    const Row<BF16> row(a, b);
-    const Wish wish = wish_of(a, b);
-    const int c0 = even_begin(row.chunks, a.S, s), c1 = even_begin(row.chunks, a.S, s + 1);
-    float top[GROUPS];
+struct Held {
+    u32x4 x[HELD];
+    __device__ __forceinline__ void load(const Row<BF16> &row, int c0, int c1)
+    {
+        // whole chunks of the row (its first and last may not be)
+        const int first = row.off ? 1 : 0, last = (row.off + row.V) / Row<BF16>::EPC - 1;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i)
-        top[i] = -INFINITY;
-    row.template each<GROUPS>(c0, c1, [&](int c, const u32x4 &x) {
-        float m = Row<BF16>::get(x, 0);
+        for (int i = 0; i < HELD; ++i) {
+            const int c = c0 + threadIdx.x + i * NT;
+            x[i] = row.nothing();
+            if (c0 + i * NT < c1 && first <= last)          // (uniform)
+                x[i] = __builtin_nontemporal_load((const u32x4 *)(row.line + (size_t)16 * min(max(c, first), last)));
+        }
 #pragma unroll
-        for (int e = 1; e < Row<BF16>::EPC; ++e)
-            m = fmaxf(m, Row<BF16>::get(x, e));
-        const int g = (c - c0) / NT % GROUPS;
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i)
-            top[i] = g == i ? fmaxf(top[i], m) : top[i];
-    });
-    float m = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i)
-        m = fmaxf(m, top[i]);
-    m = block_all(m, sm.best, [](float x, float y) { return fmaxf(x, y); });
-    Slice out = {m, -1, 0.0};
-    if (!wish.few || !(m < INFINITY))
-        return out;
+        for (int i = 0; i < HELD; ++i) {
+            const int c = c0 + threadIdx.x + i * NT;
+            if (c >= c1)
+                x[i] = row.nothing();
+            else if (c < first || c > last)
+                x[i] = row.load(c);
+        }
+    }
+};
 
-    // the border: the first of SUBS steps down to the lowest of the groups' largest that
-    // has k of them above it; if there are not k, whatever is not -inf
-    float low = INFINITY;
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i)
-        low = top[i] > -INFINITY ? fminf(low, top[i]) : low;
-    low = block_all(low, sm.low, [](float x, float y) { return fminf(x, y); });
-    const float range = m - low, step = range > 0.f && range < INFINITY ? (SUBS - 1) / range : 0.f;
-    auto level = [&](float x) { return (m - x) * step; };
+template <bool BF16>
+__device__ __forceinline__ Slice find_candidates(const SampleArgs &a, const Wish &wish, int b, int s, Shared &sm)
+{
+    using R = Row<BF16>;
+    const R row(a, b);
+    const int c0 = even_begin(row.chunks, a.S, s), c1 = even_begin(row.chunks, a.S, s + 1);
+    Held<BF16> held;
+    held.load(row, c0, c1);
     for (int i = threadIdx.x; i < SUBS; i += NT)
         sm.count[i] = 0;
     if (threadIdx.x == 0) {
         sm.n = 0;
         sm.at = SUBS;
     }
+    float top[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+        top[i] = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (c0 + i * NT < c1)                // (uniform)
+#pragma unroll
+            for (int e = 0; e < R::EPC; ++e)
+                top[i % GROUPS] = fmaxf(top[i % GROUPS], R::get(held.x[i], e));
+    float m = -INFINITY, low = INFINITY;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        m = fmaxf(m, top[i]);
+        low = top[i] > -INFINITY ? fminf(low, top[i]) : low;
+    }
+    // (both in one turn)
+    const auto max_of = [](float x, float y) { return fmaxf(x, y); };
+    const auto min_of = [](float x, float y) { return fminf(x, y); };
+    m = wave_all(m, -INFINITY, max_of);
+    low = wave_all(low, INFINITY, min_of);
+    if (threadIdx.x % 64 == 0) {
+        sm.best[threadIdx.x / 64] = m;
+        sm.low[threadIdx.x / 64] = low;
+    }
     __syncthreads();
+    m = wave_all(threadIdx.x % 64 < NWAVE ? sm.best[threadIdx.x % 64] : -INFINITY, -INFINITY, max_of);
+    low = wave_all(threadIdx.x % 64 < NWAVE ? sm.low[threadIdx.x % 64] : INFINITY, INFINITY, min_of);
+    Slice out = {m, -1, 0.0};
+    if (!wish.few || !(m < INFINITY))
+        return out;
+
+    // the border: the first of SUBS steps down to the lowest of the groups' largest that
+    // has k of them above it; if there are not k, whatever is not -inf
+    const float range = m - low, step = range > 0.f && range < INFINITY ? (SUBS - 1) / range : 0.f;
+    auto level = [&](float x) { return (m - x) * step; };
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i)
         if (top[i] > -INFINITY)
             atomicAdd(&sm.count[min((int)level(top[i]), SUBS - 1)], 1u);
+    // (meanwhile the sum of the weights)
+    const float base = m == -INFINITY ? 0.f : m, c2 = 1.44269504088896340736f / wish.T;
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+        if (c0 + i * NT < c1)
+#pragma unroll
+            for (int e = 0; e < R::EPC; ++e)
+                z += __builtin_amdgcn_exp2f((R::get(held.x[i], e) - base) * c2);
     __syncthreads();
     static_assert(SUBS == NT, "one step per thread");
     u64 all;
@@ -367,28 +464,22 @@ __device__ Slice find_candidates(const SampleArgs &a, int b, int s, Shared &sm)
     __syncthreads();
     const float border = sm.at == SUBS ? INFINITY : (float)(sm.at + 1);
     const int room = LIST / a.S;
-    const float base = m == -INFINITY ? 0.f : m, c2 = 1.44269504088896340736f / wish.T;
-    float z = 0.f;
-    row.template each<4>(c0, c1, [&](int c, const u32x4 &x) {
-        float cm = -INFINITY;
+    auto above = [&](float v) { return v > -INFINITY && (border == INFINITY || level(v) < border); };
 #pragma unroll
-        for (int e = 0; e < Row<BF16>::EPC; ++e) {
-            const float v = Row<BF16>::get(x, e);
-            cm = fmaxf(cm, v);
-            z += __builtin_amdgcn_exp2f((v - base) * c2);
-        }
-        if (cm > -INFINITY && (border == INFINITY || level(cm) < border))
+    for (int g = 0; g < GROUPS; ++g)
+        if (above(top[g]))                   // (few threads have any)
 #pragma unroll
-            for (int e = 0; e < Row<BF16>::EPC; ++e) {
-                const float v = Row<BF16>::get(x, e);
-                if (v > -INFINITY && (border == INFINITY || level(v) < border)) {
-                    const uint32_t i = atomicAdd(&sm.n, 1u);
-                    if (i < (uint32_t)room)
-                        sm.list[i].place = place_of(v, row.index(c, e));
+            for (int i = g; i < HELD; i += GROUPS)
+#pragma unroll
+                for (int e = 0; e < R::EPC; ++e) {
+                    const float v = R::get(held.x[i], e);
+                    if (above(v)) {
+                        const uint32_t n = atomicAdd(&sm.n, 1u);
+                        if (n < (uint32_t)room)
+                            sm.list[n] = place_of(v, row.index(c0 + threadIdx.x + i * NT, e));
+                    }
                 }
-            }
-    });
-    out.z = block_all((double)z, sm.z, [](double x, double y) { return x + y; });
+    out.z = block_all((double)z, 0.0, sm.z, [](double x, double y) { return x + y; });
     out.n = sm.n <= (uint32_t)room ? (int)sm.n : -1;
     return out;
 }
@@ -397,10 +488,9 @@ __device__ Slice find_candidates(const SampleArgs &a, int b, int s, Shared &sm)
 
 // sm.hist and, for a top-k, sm.count; NaN if there is one
 template <bool BF16>
-__device__ double fill_histogram(const SampleArgs &a, int b, int s, float best, Shared &sm)
+__device__ __forceinline__ double fill_histogram(const SampleArgs &a, const Wish &wish, int b, int s, float best, Shared &sm)
 {
     const Row<BF16> row(a, b);
-    const Wish wish = wish_of(a, b);
     const int c0 = even_begin(row.chunks, a.S, s), c1 = even_begin(row.chunks, a.S, s + 1);
     fill_table(sm.table);
     for (int i = threadIdx.x; i < NB; i += NT) {
@@ -447,50 +537,108 @@ struct Border {
     }
 };
 
-// The list's tokens, each compared with each: P neighbouring threads (a power of two that
-// divides a wave) take one token, every P-th of the others each.
-struct Compared {
-    u64 rank, before;    // tokens and weight of the list above this thread's
-    u64 place, w;        // of it
-    bool own;            // one of the P threads, where there is a token
-};
-
-__device__ __forceinline__ int threads_each(int n)
+// Where the border lies among the threads' tokens (one each, where `active`; `rank` tokens
+// and `before` weight lie above them all): those from place sm.cut up are within, sm.w_cut
+// is all weight to there.  `exact`: a place's weight in units.  The places' range is cut in
+// SUBS parts, the sums of the parts show in which the border lies, and so on with that
+// part until FEW tokens are left, which are compared each with each.
+template <class W>
+__device__ __forceinline__ void narrow(Shared &sm, u64 place, u64 w, bool active, u64 rank, u64 before, const Border &border, W exact)
 {
-    int p = 1;
-    while (p < 64 && 2 * p * n <= NT)
-        p *= 2;
-    return p;
-}
-
-__device__ Compared compare_list(Shared &sm, int n, const Weigher &weigh)
-{
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += NT)
-        sm.list[i].w = weigh.weight(logit_of(sm.list[i].place));
-    __syncthreads();
-    const int p = threads_each(n), i = threadIdx.x / p, part = threadIdx.x & (p - 1);
-    Compared t = {0, 0, 0, 0, i < n && part == 0};
-    if (i < n) {
-        const Token own = sm.list[i];
-        t.place = own.place;
-        t.w = own.w;
-        for (int j = part; j < n; j += p) {
-            const Token x = sm.list[j];
-            t.rank += x.place > own.place;
-            t.before += x.place > own.place ? x.w : 0;
+    for (;;) {
+        if (threadIdx.x == 0) {
+            sm.low_place = ~0ull;
+            sm.high_place = 0;
+            sm.n_few = 0;
+            sm.at = 0;
         }
-        for (int m = 1; m < p; m *= 2) {
-            t.rank += __shfl_xor(t.rank, m);
-            t.before += __shfl_xor(t.before, m);
+        sm.w[threadIdx.x] = 0;
+        sm.n_of[threadIdx.x] = 0;
+        __syncthreads();
+        const u64 low = wave_all(active ? place : ~0ull, ~0ull, [](u64 x, u64 y) { return x < y ? x : y; });
+        const u64 high = wave_all(active ? place : 0ull, 0ull, [](u64 x, u64 y) { return x > y ? x : y; });
+        const u64 mask = __builtin_amdgcn_ballot_w64(active);
+        uint32_t at = 0;
+        if (mask) {
+            if (threadIdx.x % 64 == 0) {
+                atomicMin(&sm.low_place, low);
+                atomicMax(&sm.high_place, high);
+                at = atomicAdd(&sm.n_few, (uint32_t)__builtin_popcountll(mask));
+            }
+            at = __shfl(at, 0) + __builtin_popcountll(mask & ((1ull << threadIdx.x % 64) - 1));
         }
+        if (active)
+            sm.few[at] = Token{place, w};
+        __syncthreads();
+        const int n = sm.n_few;
+        const u64 most = sm.high_place;
+        if (n <= FEW) {
+            // P neighbouring threads take a token, every P-th of the others each
+            constexpr int P = NT / FEW;
+            const int i = threadIdx.x / P, part = threadIdx.x % P;
+            Token own = {0, 0};
+            u64 above = 0;
+            uint32_t many = 0;
+            if (i < n) {
+                own = sm.few[i];
+                for (int j = part; j < n; j += P) {
+                    const Token x = sm.few[j];
+                    many += x.place > own.place;
+                    above += x.place > own.place ? x.w : 0;
+                }
+            }
+#pragma unroll
+            for (int m = 1; m < P; m *= 2) {
+                many += __shfl_xor(many, m);
+                above += __shfl_xor(above, m);
+            }
+            const bool in = i < n && part == 0 && border.in(rank + many, before + above, exact(own.place));
+            // (none: a cut above all of these, not above what was above them)
+            const auto least_of = [](u64 x, u64 y) { return x < y ? x : y; };
+            const auto sum_of = [](u64 x, u64 y) { return x + y; };
+            const u64 cut = wave_all(in ? own.place : n ? most + 1 : ~0ull, ~0ull, least_of);
+            const u64 kept = wave_all(in ? own.w : 0ull, 0ull, sum_of);
+            if (threadIdx.x % 64 == 0) {
+                sm.sum[0][threadIdx.x / 64] = cut;
+                sm.sum[1][threadIdx.x / 64] = kept;
+            }
+            __syncthreads();
+            const int lane = threadIdx.x % 64;
+            const u64 c = wave_all(lane < NWAVE ? sm.sum[0][lane] : ~0ull, ~0ull, least_of);
+            const u64 k = wave_all(lane < NWAVE ? sm.sum[1][lane] : 0ull, 0ull, sum_of);
+            if (threadIdx.x == 0) {
+                sm.cut = c;
+                sm.w_cut = before + k;
+            }
+            __syncthreads();
+            return;
+        }
+        const u64 range = most - sm.low_place;
+        const int shift = max(0, 54 - (int)__builtin_clzll(range | 1));     // range >> shift < SUBS
+        static_assert(SUBS == 1024, "54");
+        const uint32_t sub = (uint32_t)((most - place) >> shift);
+        if (active) {
+            atomicAdd(&sm.w[sub], w);
+            atomicAdd(&sm.n_of[sub], 1u);
+        }
+        __syncthreads();
+        u64 wb = sm.w[threadIdx.x], nb = sm.n_of[threadIdx.x];
+        const bool some = nb;
+        u64 all;
+        block_before2(wb, nb, sm.sum, all);
+        // (the largest weight that a place of the part could have)
+        note_last(&sm.at, some && border.in(rank + nb, before + wb, exact(most - ((u64)threadIdx.x << shift))), threadIdx.x);
+        __syncthreads();
+        if (threadIdx.x == sm.at) {
+            sm.rank = rank + nb;
+            sm.before = before + wb;
+        }
+        active &= sub == sm.at;
+        __syncthreads();
+        rank = sm.rank;
+        before = sm.before;
+        __syncthreads();
     }
-    return t;
-}
-
-__device__ __forceinline__ u64 block_sum(u64 x, Shared &sm)
-{
-    return block_all(x, sm.scan, [](u64 a, u64 b) { return a + b; });
 }
 
 // Where the border lies among the tokens of bucket b, of which `rank` tokens and `before`
@@ -498,10 +646,18 @@ __device__ __forceinline__ u64 block_sum(u64 x, Shared &sm)
 // weight to there.  Returns how many tokens sm.list holds, the whole
 // bucket, or -1 if they were too many.
 template <bool BF16>
-__device__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, int b, u64 rank, u64 before,
+__device__ __forceinline__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, int b, u64 rank, u64 before,
                         const Border &border)
 {
     uint32_t lo = 0, hi = 0xFFFFFFFFu;
+    // logits that may be in the bucket, by 32 bits
+    const double slack = 1e-6 * (fabs(weigh.best) + 31.0 / weigh.inv_T);
+    const float least_x = (float)(weigh.best - (b + 1) * BUCKET / weigh.inv_T - slack);
+    const float most_x = (float)(weigh.best - b * BUCKET / weigh.inv_T + slack);
+    auto here = [&](float v, uint32_t &key) {
+        key = order_key(v);
+        return v >= least_x && v <= most_x && key >= lo && key <= hi && weigh.bucket(v) == b;
+    };
     for (bool whole = true;; whole = false) {
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -515,17 +671,19 @@ __device__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, 
 #pragma unroll
             for (int e = 0; e < Row<BF16>::EPC; ++e) {
                 const float v = Row<BF16>::get(x, e);
-                const uint32_t key = order_key(v);
-                if (weigh.bucket(v) == b && key >= lo && key <= hi) {
+                uint32_t key;
+                if (here(v, key)) {
                     const uint32_t i = atomicAdd(&sm.n, 1u);
                     if (i < LIST)
-                        sm.list[i].place = place_of(v, row.index(c, e));
+                        sm.list[i] = place_of(v, row.index(c, e));
                     least = min(least, key);
                     most = max(most, key);
                 }
             }
         });
-        if (least <= most) {
+        least = wave_all(least, 0xFFFFFFFFu, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+        most = wave_all(most, 0u, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+        if (least <= most && threadIdx.x % 64 == 0) {
             atomicMin(&sm.lo, least);
             atomicMax(&sm.hi, most);
         }
@@ -535,15 +693,10 @@ __device__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, 
         hi = sm.hi;
         const u64 none = ((u64)hi + 1) << 32;    // a cut above all of these (not above what was above them)
         if (n <= LIST) {
-            const Compared t = compare_list(sm, (int)n, weigh);
-            const bool in = t.own && border.in(rank + t.rank, before + t.before, weigh.exact(logit_of(t.place)));
-            const u64 upto = before + block_sum(in ? t.w : 0, sm);
-            const u64 cut = block_all(in ? t.place : none, sm.scan, [](u64 x, u64 y) { return x < y ? x : y; });
-            if (threadIdx.x == 0) {
-                sm.cut = cut;
-                sm.w_cut = upto;
-            }
-            __syncthreads();
+            const bool active = threadIdx.x < n;
+            const u64 place = active ? sm.list[threadIdx.x] : 0;
+            narrow(sm, place, active ? weigh.weight(logit_of(place)) : 0, active, rank, before, border,
+                   [&](u64 p) { return weigh.exact(logit_of(p)); });
             return whole ? (int)n : -1;
         }
         if (lo == hi) {
@@ -593,7 +746,7 @@ __device__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, 
         const uint32_t step = (hi - lo) / SUBS + 1;
         for (int i = threadIdx.x; i < SUBS; i += NT) {
             sm.w[i] = 0;
-            sm.w[SUBS + i] = 0;
+            sm.n_of[i] = 0;
         }
         if (threadIdx.x == 0)
             sm.at = 0;
@@ -602,20 +755,20 @@ __device__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, 
 #pragma unroll
             for (int e = 0; e < Row<BF16>::EPC; ++e) {
                 const float v = Row<BF16>::get(x, e);
-                const uint32_t key = order_key(v);
-                if (weigh.bucket(v) == b && key >= lo && key <= hi) {
+                uint32_t key;
+                if (here(v, key)) {
                     atomicAdd(&sm.w[(hi - key) / step], weigh.weight(v));
-                    atomicAdd(&sm.w[SUBS + (hi - key) / step], 1ull);
+                    atomicAdd(&sm.n_of[(hi - key) / step], 1u);
                 }
             }
         });
         __syncthreads();
+        u64 wb = sm.w[threadIdx.x], nb = sm.n_of[threadIdx.x];
+        const bool some = nb;
         u64 all;
-        const u64 wb = block_before(sm.w[threadIdx.x], sm.scan, all);
-        const u64 nb = block_before(sm.w[SUBS + threadIdx.x], sm.scan, all);
+        block_before2(wb, nb, sm.sum, all);
         const uint32_t key = hi - threadIdx.x * step;    // the part's largest, if it is one
-        if (sm.w[SUBS + threadIdx.x] && border.in(rank + nb, before + wb, weigh.exact(logit_of((u64)key << 32))))
-            atomicMax(&sm.at, threadIdx.x);
+        note_last(&sm.at, some && border.in(rank + nb, before + wb, weigh.exact(logit_of((u64)key << 32))), threadIdx.x);
         __syncthreads();
         if (threadIdx.x == sm.at) {
             sm.slice[0] = wb;
@@ -640,10 +793,9 @@ __device__ __forceinline__ u64 goal_of(float u, u64 total)
 }
 
 template <bool BF16, bool ONE>
-__device__ void choose_token(const SampleArgs &a, int b, Shared &sm, Slice one)
+__device__ __forceinline__ void choose_token(const SampleArgs &a, const Wish &wish, int b, Shared &sm, Slice one)
 {
     const Row<BF16> row(a, b);
-    const Wish wish = wish_of(a, b);
     const int S = ONE ? 1 : a.S;
     float best = one.top;
     bool few = one.n >= 0;
@@ -668,62 +820,99 @@ __device__ void choose_token(const SampleArgs &a, int b, Shared &sm, Slice one)
         }
         return;
     }
-    const float u = a.u[b];
     const Weigher weigh = {best, 1.0 / (double)wish.T, sm.table};
-    if (!ONE || few)
-        fill_table(sm.table);
     int token;
     if (few) {
-        int n = one.n;
-        if (!ONE) {
-            n = 0;
+        // a token a thread
+        u64 place = 0;
+        bool active = false;
+        if (ONE) {
+            active = (int)threadIdx.x < one.n;
+            place = sm.list[threadIdx.x];
+        } else {
+            int n = 0;
             for (int s = 0; s < S; ++s) {
-                const int ns = slice_at(a, b, s)->n;
-                for (int i = threadIdx.x; i < ns; i += NT)
-                    sm.list[n + i].place = a.lists[((size_t)b * S + s) * (LIST / S) + i];
+                const int ns = slice_at(a, b, s)->n, i = (int)threadIdx.x - n;
+                if (i >= 0 && i < ns) {
+                    active = true;
+                    place = a.lists[((size_t)b * S + s) * (LIST / S) + i];
+                }
                 n += ns;
             }
         }
+        auto exact = [&](u64 p) { return exp((double)(logit_of(p) - best) * weigh.inv_T) * UNIT; };
+        const u64 w = active ? (u64)(exact(place) + 0.5) : 0;
+        // by top-k alone, for the weight that top_p is a part of (of no account without it); then by all
+        Border border = {(u64)wish.k, INFINITY, 0.0};
+        for (int turn = wish.p < 1.0 ? 0 : 1; turn < 2; ++turn) {
+            if (turn == 1) {
+                border.w = wish.p < 1.0 ? wish.p * (double)sm.w_cut : wish.p >= 1.0 ? INFINITY : 0.0;
+                border.least = wish.min_p * UNIT;
+                __syncthreads();
+            }
+            narrow(sm, place, w, active, 0, 0, border, exact);
+        }
+        const u64 goal = goal_of(wish.u, sm.w_cut);
+        active &= place >= sm.cut;
+        // the part of the indexes that the goal lies in, and the token in it
+        const int shift = max(0, 22 - (int)__builtin_clz((uint32_t)a.V));   // V >> shift < SUBS
+        const int index = index_of(place);
+        sm.w[threadIdx.x] = 0;
+        if (threadIdx.x == 0) {
+            sm.n_few = 0;
+            sm.found = 0;
+        }
         __syncthreads();
-        const Compared t = compare_list(sm, n, weigh);
-        const u64 total = block_sum(t.own && t.rank < (u64)wish.k ? t.w : 0, sm);
-        const Border border = {(u64)wish.k, wish.p * (double)total, wish.min_p * UNIT};
-        const bool in = t.own && border.in(t.rank, t.before, weigh.exact(logit_of(t.place)));
-        const u64 kept = block_sum(in ? t.w : 0, sm), goal = goal_of(u, kept);
-        // the kept tokens' weights by index: again each with each
-        const int p = threads_each(n), i = threadIdx.x / p;
-        if (t.own)
-            sm.list[i].w = in ? t.w : 0;
+        if (active)
+            atomicAdd(&sm.w[index >> shift], w);
         __syncthreads();
-        if (i < n) {
-            u64 at = 0;
-            for (int j = threadIdx.x & (p - 1); j < n; j += p)
-                at += index_of(sm.list[j].place) < index_of(t.place) ? sm.list[j].w : 0;
-            for (int m = 1; m < p; m *= 2)
-                at += __shfl_xor(at, m);
-            if (in && at <= goal && goal < at + t.w)
-                sm.found = index_of(t.place);
+        u64 all;
+        const u64 part = sm.w[threadIdx.x], sum = block_before(part, sm.scan, all);
+        if (sum <= goal && goal < sum + part) {
+            sm.at = threadIdx.x;
+            sm.before = sum;
+        }
+        __syncthreads();
+        active &= (uint32_t)index >> shift == sm.at;
+        if (active)
+            sm.few[atomicAdd(&sm.n_few, 1u)] = Token{place, w};
+        __syncthreads();
+        if (active) {
+            u64 at = sm.before;
+            for (uint32_t j = 0; j < sm.n_few; ++j)
+                at += index_of(sm.few[j].place) < index ? sm.few[j].w : 0;
+            if (at <= goal && goal < at + w)
+                sm.found = index;
         }
         __syncthreads();
         token = sm.found;
     } else {
-        if (!ONE)
+        const bool counted = wish.k < a.V;
+        if (!ONE) {
+            fill_table(sm.table);
+            const u64 *weights = a.weights + (size_t)b * S * NB;
+            const uint32_t *counts = a.counts + (size_t)b * S * NB;
             for (int i = threadIdx.x; i < NB; i += NT) {
                 u64 w = 0;
                 uint32_t n = 0;
-                for (int s = 0; s < S; ++s) {
-                    w += a.weights[((size_t)b * S + s) * NB + i];
-                    n += a.counts[((size_t)b * S + s) * NB + i];
-                }
+#pragma unroll 8
+                for (int s = 0; s < S; ++s)
+                    w += weights[s * NB + i];
+                if (counted)
+#pragma unroll 8
+                    for (int s = 0; s < S; ++s)
+                        n += counts[s * NB + i];
                 sm.hist[i] = w;
                 sm.count[i] = n;
             }
+        }
         __syncthreads();
         // two buckets a thread: what lies before them
         const int i0 = 2 * threadIdx.x;
         u64 all, total;
-        const u64 n0 = block_before((u64)sm.count[i0] + sm.count[i0 + 1], sm.scan, all), n1 = n0 + sm.count[i0];
-        const u64 w0 = block_before(sm.hist[i0] + sm.hist[i0 + 1], sm.scan, total), w1 = w0 + sm.hist[i0];
+        u64 n0 = (u64)sm.count[i0] + sm.count[i0 + 1], w0 = sm.hist[i0] + sm.hist[i0 + 1];
+        block_before2(n0, w0, sm.sum, total);
+        const u64 n1 = n0 + sm.count[i0], w1 = w0 + sm.hist[i0];
         z = (double)total / UNIT;
         // the last bucket that holds a token within the border (the first does), and what
         // is before it: in sm.at, sm.slice[0] and sm.slice[1]
@@ -733,10 +922,8 @@ __device__ void choose_token(const SampleArgs &a, int b, Shared &sm, Slice one)
                 sm.at = 0;
             __syncthreads();
             // (a bucket's own weight: that of its lower end, the largest)
-            if (border.in(n0, w0, sm.table[i0]))
-                atomicMax(&sm.at, (uint32_t)i0);
-            if (border.in(n1, w1, sm.table[i0 + 1]))
-                atomicMax(&sm.at, (uint32_t)i0 + 1);
+            const bool in0 = border.in(n0, w0, sm.table[i0]), in1 = border.in(n1, w1, sm.table[i0 + 1]);
+            note_last(&sm.at, in0 || in1, (uint32_t)i0 + in1);
             __syncthreads();
             if (i0 == ((int)sm.at & ~1)) {
                 sm.slice[0] = sm.at & 1 ? n1 : n0;
@@ -744,52 +931,58 @@ __device__ void choose_token(const SampleArgs &a, int b, Shared &sm, Slice one)
             }
             __syncthreads();
         };
-        Border border = {(u64)1 << 62, INFINITY, 0.0};
-        u64 kept = total;            // by top-k
-        if (wish.k < a.V) {
-            border.k = wish.k;
+        // by top-k alone, for the weight that top_p is a part of; then by all
+        Border border = {counted ? (u64)wish.k : (u64)1 << 62, INFINITY, 0.0};
+        u64 kept = total, cut = ~0ull;
+        int at = NB - 1, listed = 0;
+        for (int turn = counted ? 0 : 1; turn < 2; ++turn) {
+            if (turn == 1) {
+                border.w = wish.p * (double)kept;
+                border.least = wish.min_p * UNIT;
+            }
             last_bucket(border);
-            const int at = sm.at;
-            const u64 rank = sm.slice[0], before = sm.slice[1];
+            at = sm.at;
+            kept = total;
             if (at < NB - 1) {
-                find_cut(row, sm, weigh, at, rank, before, border);
+                const u64 rank = sm.slice[0], before = sm.slice[1];
+                listed = find_cut(row, sm, weigh, at, rank, before, border);
+                cut = sm.cut;
                 kept = sm.w_cut;
             }
         }
-        border.w = wish.p * (double)kept;
-        border.least = wish.min_p * UNIT;
-        last_bucket(border);
-        const int at = sm.at;
-        const u64 rank = sm.slice[0], before = sm.slice[1];
-        u64 cut = ~0ull;
-        kept = total;
-        int listed = 0;
-        if (at < NB - 1) {
-            listed = find_cut(row, sm, weigh, at, rank, before, border);
-            cut = sm.cut;
-            kept = sm.w_cut;
-        }
-        auto weight_in = [&](float x, int i) {
+        const float least_x =         // (what is surely lower has no weight here)
+            (float)(best - (at + 1) * BUCKET * wish.T - 1e-6 * (fabs((double)best) + 31.0 * wish.T));
+        auto weight_in = [&](float x, int i) -> u64 {
+            if (!(x >= least_x))
+                return 0;
             double r;
             const int k = weigh.bucket(x, r);
             return k < at || (k == at && k < NB - 1 && place_of(x, i) >= cut) ? weigh.rounded(k, r) : 0;
         };
         // the slice that the goal lies in, from the slices' sums
-        u64 goal = goal_of(u, kept);
+        u64 goal = goal_of(wish.u, kept);
         int s = 0;
         if (!ONE) {
             __syncthreads();
             if (threadIdx.x < MAX_SLICES)
                 sm.slice[threadIdx.x] = 0;
             __syncthreads();
-            for (int i = threadIdx.x; i < S * NB; i += NT)
-                if (i % NB < at)
-                    atomicAdd(&sm.slice[i / NB], a.weights[((size_t)b * S + i / NB) * NB + i % NB]);
+            for (int i = threadIdx.x / 64; i < S; i += NWAVE) {       // a wave to a slice
+                const u64 *const w = a.weights + ((size_t)b * S + i) * NB;
+                u64 sum = 0;
+#pragma unroll 8
+                for (int j = threadIdx.x % 64; j < at; j += 64)
+                    sum += w[j];
+                sum = wave_all(sum, (u64)0, [](u64 x, u64 y) { return x + y; });
+                if (threadIdx.x % 64 == 0)
+                    atomicAdd(&sm.slice[i], sum);
+            }
             if (listed >= 0) {
-                for (int i = threadIdx.x; i < listed; i += NT)
-                    if (sm.list[i].place >= cut)
-                        atomicAdd(&sm.slice[even_part_of(row.chunks, S, (index_of(sm.list[i].place) + row.off) / Row<BF16>::EPC)],
-                                  sm.list[i].w);
+                if ((int)threadIdx.x < listed && sm.list[threadIdx.x] >= cut) {
+                    const u64 place = sm.list[threadIdx.x];
+                    atomicAdd(&sm.slice[even_part_of(row.chunks, S, (index_of(place) + row.off) / Row<BF16>::EPC)],
+                              weigh.weight(logit_of(place)));
+                }
             } else
                 row.template each<2>(0, row.chunks, [&](int c, const u32x4 &x) {
 #pragma unroll
@@ -845,12 +1038,13 @@ __global__ __launch_bounds__(NT) void sample_one_kernel(SampleArgs a)
 {
     __shared__ Shared sm;
     const int b = blockIdx.x;
-    Slice one = find_candidates<BF16>(a, b, 0, sm);
+    const Wish wish = wish_of(a, b);
+    Slice one = find_candidates<BF16>(a, wish, b, 0, sm);
     __syncthreads();
     if (one.n < 0 && one.top > -INFINITY && one.top < INFINITY)
-        one.z = fill_histogram<BF16>(a, b, 0, one.top, sm);
+        one.z = fill_histogram<BF16>(a, wish, b, 0, one.top, sm);
     __syncthreads();
-    choose_token<BF16, true>(a, b, sm, one);
+    choose_token<BF16, true>(a, wish, b, sm, one);
 }
 
 template <bool BF16>
@@ -858,9 +1052,9 @@ __global__ __launch_bounds__(NT) void sample_candidates_kernel(SampleArgs a)
 {
     __shared__ Shared sm;
     const int b = blockIdx.x / a.S, s = blockIdx.x % a.S;
-    const Slice x = find_candidates<BF16>(a, b, s, sm);
+    const Slice x = find_candidates<BF16>(a, wish_of(a, b), b, s, sm);
     for (int i = threadIdx.x; i < x.n; i += NT)
-        a.lists[((size_t)b * a.S + s) * (LIST / a.S) + i] = sm.list[i].place;
+        a.lists[((size_t)b * a.S + s) * (LIST / a.S) + i] = sm.list[i];
     if (threadIdx.x == 0)
         *slice_at(a, b, s) = x;
 }
@@ -878,10 +1072,13 @@ __global__ __launch_bounds__(NT) void sample_histogram_kernel(SampleArgs a)
     }
     if (few || !(best > -INFINITY && best < INFINITY))
         return;
-    const double z = fill_histogram<BF16>(a, b, s, best, sm);
+    const Wish wish = wish_of(a, b);
+    const double z = fill_histogram<BF16>(a, wish, b, s, best, sm);
+    const bool counted = wish.k < a.V;
     for (int i = threadIdx.x; i < NB; i += NT) {
         a.weights[((size_t)b * a.S + s) * NB + i] = sm.hist[i];
-        a.counts[((size_t)b * a.S + s) * NB + i] = sm.count[i];
+        if (counted)
+            a.counts[((size_t)b * a.S + s) * NB + i] = sm.count[i];
     }
     if (threadIdx.x == 0)
         slice_at(a, b, s)->z = z;
@@ -891,16 +1088,18 @@ template <bool BF16>
 __global__ __launch_bounds__(NT) void sample_choose_kernel(SampleArgs a)
 {
     __shared__ Shared sm;
-    choose_token<BF16, false>(a, blockIdx.x, sm, Slice{});
+    choose_token<BF16, false>(a, wish_of(a, blockIdx.x), blockIdx.x, sm, Slice{});
 }
 
 // Slices of a row: one workgroup takes rows of up to 32768 logits, and any where there
-// are rows for half of the CUs
-int slices_of(int B, int V)
+// are rows for half of the CUs; a slice has HELD NT chunks of 16 bytes at most (a row
+// touches up to two more than it has bytes for)
+int slices_of(int B, int V, int per_chunk = 4)
 {
+    const int least = (V / per_chunk + 2 + HELD * NT - 1) / (HELD * NT);
     if (V <= 32768 || B >= 128)
-        return 1;
-    return std::max(1, std::min(std::min(512 / B, V / 8192), MAX_SLICES));
+        return least;
+    return std::max(least, std::min(std::min(512 / B, V / 8192), MAX_SLICES));
 }
 
 struct Workspace {
@@ -952,7 +1151,7 @@ ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const fl
     for (const Span &s : in)
         if (overlaps(out[0], s) || overlaps(out[1], s))
             return TA_ERR_ALIASING;
-    const Workspace w = workspace_of(B, V);
+    const Workspace w = workspace_of(B, V);        // (enough for either type)
     if (w.all) {
         if (!workspace || workspace_bytes < w.all)
             return TA_ERR_WORKSPACE;
@@ -966,7 +1165,7 @@ ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const fl
                 return TA_ERR_ALIASING;
     }
     unsigned char *const ws = (unsigned char *)workspace;
-    const SampleArgs a = {logits, stride, u, temperature, top_k, top_p, min_p, token, logp, V, slices_of(B, V),
+    const SampleArgs a = {logits, stride, u, temperature, top_k, top_p, min_p, token, logp, V, slices_of(B, V, l_bf16 ? 8 : 4),
                           (Slice *)(ws + w.slices), (u64 *)(ws + w.lists), (u64 *)(ws + w.weights),
                           (uint32_t *)(ws + w.counts)};
     hipStream_t s = (hipStream_t)stream;
