@@ -252,18 +252,18 @@ struct Row {
     template <int U, class F>
     __device__ __forceinline__ void each(int c0, int c1, F f) const
     {
-        int c = c0 + threadIdx.x;
-        for (; c + (U - 1) * NT < c1; c += U * NT) {
+        for (int base = c0; base < c1; base += U * NT) {
+            const int c = base + threadIdx.x;
             u32x4 x[U];
 #pragma unroll
             for (int i = 0; i < U; ++i)
-                x[i] = load(c + i * NT);
+                if (base + i * NT < c1)          // (uniform)
+                    x[i] = c + i * NT < c1 ? load(c + i * NT) : nothing();
 #pragma unroll
             for (int i = 0; i < U; ++i)
-                f(c + i * NT, x[i]);
+                if (c + i * NT < c1)
+                    f(c + i * NT, x[i]);
         }
-        for (; c < c1; c += NT)
-            f(c, load(c));
     }
 };
 
@@ -471,7 +471,7 @@ __device__ __forceinline__ Slice find_candidates(const SampleArgs &a, const Wish
 #pragma unroll
             for (int i = g; i < HELD; i += GROUPS)
 #pragma unroll
-                for (int e = 0; e < R::EPC; ++e) {
+                for (int e = 0; e < R::EPC && c0 + i * NT < c1; ++e) {
                     const float v = R::get(held.x[i], e);
                     if (above(v)) {
                         const uint32_t n = atomicAdd(&sm.n, 1u);
@@ -592,7 +592,7 @@ __device__ __forceinline__ void narrow(Shared &sm, u64 place, u64 w, bool active
                 many += __shfl_xor(many, m);
                 above += __shfl_xor(above, m);
             }
-            const bool in = i < n && part == 0 && border.in(rank + many, before + above, exact(own.place));
+            const bool in = i < n && part == 0 && border.in(rank + many, before + above, border.least > 0.0 ? exact(own.place) : 0.0);
             // (none: a cut above all of these, not above what was above them)
             const auto least_of = [](u64 x, u64 y) { return x < y ? x : y; };
             const auto sum_of = [](u64 x, u64 y) { return x + y; };
@@ -627,7 +627,8 @@ __device__ __forceinline__ void narrow(Shared &sm, u64 place, u64 w, bool active
         u64 all;
         block_before2(wb, nb, sm.sum, all);
         // (the largest weight that a place of the part could have)
-        note_last(&sm.at, some && border.in(rank + nb, before + wb, exact(most - ((u64)threadIdx.x << shift))), threadIdx.x);
+        note_last(&sm.at, some && border.in(rank + nb, before + wb,
+                                             border.least > 0.0 ? exact(most - ((u64)threadIdx.x << shift)) : 0.0), threadIdx.x);
         __syncthreads();
         if (threadIdx.x == sm.at) {
             sm.rank = rank + nb;
