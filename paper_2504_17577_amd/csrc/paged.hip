@@ -250,12 +250,20 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 // 75-78 us (6.0-6.3 TB/s), B=1 Sk=100001 of 8 bits 36 us (5.7 TB/s); of 8 bits and 64
 // dims (16 x 32 heads, 2001 positions) 31 us (4.3 TB/s: a wave's 32 keys are a quarter
 // of the bytes in flight, and the softmax's work per key is the same).
+//
+// Of 4 bits (MXFP4) a lane's 16 bytes of a K row (8 with 64 dims) are one group's, four
+// operands of the scores with one scale; of V it loads the same 8 (4) dims of its keys and
+// makes pairs of neighbouring dims of a key into bf16, scale included, then pairs of keys by
+// byte permutes; the scales of a lane's four keys come from the four lanes that loaded them.
+// The vector ALU bounds it (about 140 instructions per 16 keys of a wave, half the time on
+// each SIMD) and the loads' way, which two or three waves on a SIMD do not hide: 64 sequences of up to 16384 mixed 34 us (3.7 TB/s), B=1 Sk=100001 25 us (4.3 TB/s).
+// Tried: 64 keys a step (195 registers, two workgroups a CU: 54 us and 35 with the merge
+// instead of 40 and 32), loads two steps ahead (217 registers: 46 and 33).
 template <int D, int TYPE, int RT>
 __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 {
     constexpr bool E4M3 = TYPE == TA_CACHE_E4M3, MX = TYPE == TA_CACHE_MXFP4;
     constexpr int KB = 2;                        // 16-key blocks per wave and step
-    constexpr int AHEAD = 1;                     // steps that loads are ahead
     constexpr int KS = 16 * KB;
     constexpr int KK = D / 32;                   // k-steps of the scores
     constexpr int ROW = MX ? D / 2 : D * (E4M3 ? 1 : 2);   // bytes of a key
@@ -347,23 +355,21 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 page[kb] = table[min(((first + s * KS) >> 4) + kb, last_block) >> (a.page_shift - 4)];
         };
         size_t at[KB];             // (MXFP4: the rows before it)
-        bool bad[KB], next_bad[AHEAD][KB];
-        auto place = [&](int s, int buf) {
+        bool bad[KB], next_bad[KB];
+        auto place = [&](int s) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const int pg = paged_checked(page[kb], a.num_pages);
                 const int blk = min(((first + s * KS) >> 4) + kb, last_block);
                 const int in = (blk << 4) & ((1 << a.page_shift) - 1);
                 at[kb] = ((((size_t)max(pg, 0) * a.Hkv + h) << a.page_shift) + in) * (MX ? 1 : ROW);
-                next_bad[buf][kb] = pg < 0;
+                next_bad[kb] = pg < 0;
             }
         };
-        u32x4 k_buf[AHEAD][KB][KL];
-        uint32_t v_buf[AHEAD][KB][4][VW];
-        uint32_t kx_buf[AHEAD][KB], vx_buf[AHEAD][KB];   // MXFP4: a key's scales
-        auto load_k = [&](int buf) {
-            auto &kr = k_buf[buf];
-            auto &kx = kx_buf[buf];
+        u32x4 kr[KB][KL];
+        uint32_t vr[KB][4][VW];
+        uint32_t kx[KB], vx[KB];   // MXFP4: a key's scales
+        auto load_k = [&]() {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const unsigned char *p = (const unsigned char *)a.K + at[kb] * (MX ? ROW : 1);
@@ -386,9 +392,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 }
             }
         };
-        auto load_v = [&](int buf) {
-            auto &vr = v_buf[buf];
-            auto &vx = vx_buf[buf];
+        auto load_v = [&]() {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
                 const unsigned char *p = (const unsigned char *)a.V + at[kb] * (MX ? ROW : 1);
@@ -418,22 +422,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             }
         };
 
-        if (steps > 0)
+        if (steps > 0) {
             lookup(0);
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (i < steps) {
-                place(i, i);
-                load_k(i);
-                load_v(i);
-                if (i + 1 < steps)
-                    lookup(i + 1);
-            }
+            place(0);
+            load_k();
+            load_v();
+            if (steps > 1)
+                lookup(1);
+        }
         // `tail`: whether there are keys past the last in the step (uniform)
-        auto step = [&](int s, auto buf_of, auto tail) {
-            constexpr int buf = buf_of;
-            auto &kr = k_buf[buf];
-            auto &vr = v_buf[buf];
+        auto step = [&](int s, auto tail) {
             const int key0 = first + s * KS;
             // The K loads took whole lines of eight rows each (halves of sixteen rows'
             // lines would come from HBM twice); lanes c16 and c16 ^ 8 exchange what the
@@ -461,7 +459,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                     for (int kk = 0; kk < KK; ++kk) {
                         bf16x8 k;
                         if constexpr (MX) {
-                            k = tileattn_mx::eight(kr[kb][0][kk], tileattn_mx::scale_of(kx_buf[buf][kb]));
+                            k = tileattn_mx::eight(kr[kb][0][kk], tileattn_mx::scale_of(kx[kb]));
                         } else if constexpr (E4M3) {
                             const uint32_t w0 = kr[kb][kk >> 1][2 * (kk & 1)], w1 = kr[kb][kk >> 1][2 * (kk & 1) + 1];
                             k = __builtin_bit_cast(bf16x8, u32x4{e4m3_bf16<false>(w0), e4m3_bf16<true>(w0),
@@ -474,12 +472,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                 }
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-                bad[kb] = next_bad[buf][kb];
-            if (s + AHEAD < steps) {
-                place(s + AHEAD, buf);
-                load_k(buf);
-                if (s + AHEAD + 1 < steps)
-                    lookup(s + AHEAD + 1);
+                bad[kb] = next_bad[kb];
+            if (s + 1 < steps) {
+                place(s + 1);
+                load_k();
+                if (s + 2 < steps)
+                    lookup(s + 2);
             }
             // a page outside the pool makes its keys' scores NaN, and so the row
 #pragma unroll
@@ -495,7 +493,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             if constexpr (MX) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb) {
-                    const int x = (int)(((vx_buf[buf][kb] >> (8 * (c16 * XG / 16))) & 0xFF) << 23);
+                    const int x = (int)(((vx[kb] >> (8 * (c16 * XG / 16))) & 0xFF) << 23);
                     vsc[kb][0] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0x00, 0xF, 0xF, true));
                     vsc[kb][1] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0x55, 0xF, 0xF, true));
                     vsc[kb][2] = __uint_as_float(__builtin_amdgcn_mov_dpp(x, 0xAA, 0xF, 0xF, true));
@@ -607,20 +605,19 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                         }
                 }
             }
-            if (s + AHEAD < steps)
-                load_v(buf);
+            if (s + 1 < steps)
+                load_v();
         };
-        typedef std::integral_constant<int, 0> Even;
         if constexpr (MX) {
             // the last step by itself: the masks in every step, for the last one's sake, were a
             // sixth of the vector instructions
             for (int s = 0; s + 1 < steps; ++s)
-                step(s, Even{}, std::false_type{});
+                step(s, std::false_type{});
             if (steps > 0)
-                step(steps - 1, Even{}, std::true_type{});
+                step(steps - 1, std::true_type{});
         } else {
             for (int s = 0; s < steps; ++s)
-                step(s, Even{}, first + (s + 1) * KS > k_hi);
+                step(s, first + (s + 1) * KS > k_hi);
         }
 
         // The waves' sums meet in LDS, in wave order.  Lane: row c16, dims

@@ -103,8 +103,10 @@ __device__ __forceinline__ void normed_rotated(const RopeArgs &a, int ch, const 
 // Queries and what a bf16 cache takes are computed in 32 bits.  Keys for 8 and 4 bits
 // are computed in 64 and rounded to 32 bits once before they meet the cache's type: a
 // key next to the border of two of its numbers (a quarter of the value apart in 4 bits)
-// falls where the exact one does.  HBM bounds a prefill, the loads one behind the other
-// (seq and pos, the table, then the row) a few tokens.
+// falls where the exact one does.  HBM bounds a prefill
+// (16384 tokens of 32 + 8 + 8 heads of 128 dims into bf16, 411 MB both ways: 72 us, 5.7 TB/s,
+// the rate of a copy), the loads one behind the other (seq and pos, the table, then the row)
+// a few tokens (32: 3.3 us; 2047 into 4 bits 14, of a floor of 9).
 template <int D, int TYPE, bool INTER>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a)
 {
