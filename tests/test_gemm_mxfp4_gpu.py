@@ -38,7 +38,7 @@ SIZES = [
     # (M, N, K): few rows in blocks of 16, strips of 16, 32 and 64 columns, K in parts of steps
     (1, 8, 32), (1, 4096, 4096), (1, 72, 992), (2, 64, 64), (5, 136, 288), (16, 128, 512), (17, 1000, 1056),
     (24, 2048, 1024), (32, 256, 4096), (33, 520, 96), (48, 4096, 256), (64, 136, 2080), (49, 8, 3200),
-    (3, 8200, 160), (40, 8208, 224), (64, 16400, 128), (20, 20008, 96), (64, 17000, 416),
+    (3, 8200, 160), (9, 6152, 640), (16, 12296, 2080), (7, 10248, 2176), (40, 8208, 224), (64, 16400, 128), (20, 20008, 96), (64, 17000, 416),
     # tiles: one row over, one short, columns and K in parts
     (65, 200, 544), (96, 1024, 1024), (127, 136, 128), (128, 128, 64), (129, 264, 352), (200, 1000, 992),
     (256, 256, 256), (300, 8, 32), (389, 520, 1056), (513, 1032, 224), (130, 2056, 3200),
@@ -96,6 +96,40 @@ def test_one_weight_at_a_time(ta, M):
         a[torch.arange(M), torch.from_numpy(cols)] = 1
         got = ta.gemm_mxfp4_epilogue(a.cuda(), w.cuda(), s.cuda())
         np.testing.assert_array_equal(f64(got), v[:, cols].T)
+
+
+@pytest.mark.parametrize("M,N,K", [(300, 12296, 1056), (1021, 4232, 8224), (700, 8200, 2080), (65, 20000, 96)])
+def test_large_tiles(ta, M, N, K):
+    """Sizes at which tiles of 256 columns are chosen, and others; the oracle's arithmetic on
+    the GPU (float64)."""
+    g = torch.Generator().manual_seed(N)
+    a, (w, s, v) = torch.randn(M, K, generator=g).to(BF16).cuda(), weights(N, K, g)
+    bias, r = torch.randn(N, generator=g).to(BF16).cuda(), torch.randn(M, N, generator=g).to(BF16).cuda()
+    v = torch.from_numpy(v.T.copy()).cuda()
+    x = a.double() @ v + bias.double()
+    size = a.double().abs() @ v.abs() + bias.double().abs()
+    y = x * torch.sigmoid(x)
+    # as oracle.serving.gemm_epilogue's, and half a step of bf16
+    tol = 1.13 * (K + 2) * 2.0 ** -24 * size + 2.0 ** -20 * y.abs() + (2.0 ** -24 + 2.0 ** -8) * (y + r.double()).abs() + 1e-30
+    for parts in (None, 0, 37, 256, 512):
+        got = ta.gemm_mxfp4_epilogue(a, w, s, bias=bias, activation="silu", residual=r, out_dtype=BF16, num_parts=parts)
+        err = (got.double() - y - r.double()).abs()
+        print(f"  parts {parts}: of bound {float((err / tol).max()):.2f}", flush=True)
+        assert (err <= tol).all()
+
+
+@pytest.mark.parametrize("M", [5, 24, 60])
+def test_scales_at_any_address(ta, M):
+    """K in whole steps, the scales at each byte of a dword."""
+    N, K = 10304, 2304
+    g = torch.Generator().manual_seed(M)
+    a, (w, s, _) = torch.randn(M, K, generator=g).to(BF16).cuda(), weights(N, K, g)
+    want = ta.gemm_mxfp4_epilogue(a, w, s)
+    room = torch.zeros(N * K // 32 + 8, dtype=U8, device="cuda")
+    for at in range(1, 4):
+        t = room[at:at + N * K // 32].view(N, K // 32)
+        t.copy_(s)
+        assert torch.equal(ta.gemm_mxfp4_epilogue(a, w, t), want)
 
 
 @pytest.mark.parametrize("M", [1, 40, 300])

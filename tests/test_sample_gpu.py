@@ -90,6 +90,22 @@ def test_a_wish_for_each_row(ta):
     compare(ta, x[:, :3000].contiguous(), u, T, np.minimum(k, 2 ** 20), p, m)
 
 
+@pytest.mark.parametrize("B,V,dtype", [(2, 1 << 20, F32), (2, 1 << 20, BF16), (131, 150001, F32), (129, 139264, BF16), (128, 139265, BF16)])
+def test_largest_rows(ta, B, V, dtype):
+    """Rows that have to be cut in slices however many there are; the largest allowed.  The
+    oracle takes a few of them."""
+    for k, p, m in ((50, 0.9, None), (None, 0.9, None), (2500, None, 0.001)):
+        x, u, _ = logits(B, V, dtype, V + (k or 0))
+        some = lambda v, t=F32: None if v is None else col([v] * B, t)     # noqa: E731
+        token, logp = ta.sample_logits(x, col(u), None, some(k, I32), some(p), some(m))
+        for b in (0, B // 2, B - 1):
+            args = [0 if k is None else k] + [d if v is None else float(np.float32(v)) for v, d in ((p, INF), (m, 0.0))]
+            want, lps = ms.sample(x[b].double().cpu().numpy(), float(u[b]), 1.0, *args, V * 2.0 ** -43)
+            assert int(token[b]) in want and len(want) <= 2
+            lp = lps[want.index(int(token[b]))]
+            assert abs(float(logp[b]) - lp) <= 260 * 2.0 ** -24 + 2.0 ** -24 * abs(lp)
+
+
 @pytest.mark.parametrize("V", [1000, 30000, 100001])
 def test_masked_rows(ta, V):
     """-inf in all but a few places, in whole slices, and everywhere; NaN and +inf."""
