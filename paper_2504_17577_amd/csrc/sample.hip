@@ -653,7 +653,7 @@ __device__ __forceinline__ void narrow(Shared &sm, u64 place, u64 w, bool active
 // Where the border lies among the tokens of bucket b, of which `rank` tokens and `before`
 // weight lie above: the tokens of it from place sm.cut up are within, sm.w_cut is the
 // weight to there.  Returns how many tokens sm.list holds, the whole
-// bucket, or -1 if they were too many.
+// bucket and maybe some at its ends that are not of it, or -1 if they were too many.
 template <bool BF16>
 __device__ __forceinline__ int find_cut(const Row<BF16> &row, Shared &sm, const Weigher &weigh, int b, u64 rank, u64 before,
                         const Border &border)
@@ -667,7 +667,33 @@ __device__ __forceinline__ int find_cut(const Row<BF16> &row, Shared &sm, const 
         key = order_key(v);
         return v >= least_x && v <= most_x && key >= lo && key <= hi && weigh.bucket(v) == b;
     };
-    for (bool whole = true;; whole = false) {
+    // the whole bucket, by 32 bits alone: each thread then looks at its own token again
+    __syncthreads();
+    if (threadIdx.x == 0)
+        sm.n = 0;
+    __syncthreads();
+    row.template each<4>(0, row.chunks, [&](int c, const u32x4 &x) {
+#pragma unroll
+        for (int e = 0; e < Row<BF16>::EPC; ++e) {
+            const float v = Row<BF16>::get(x, e);
+            if (v >= least_x && v <= most_x) {
+                const uint32_t i = atomicAdd(&sm.n, 1u);
+                if (i < LIST)
+                    sm.list[i] = place_of(v, row.index(c, e));
+            }
+        }
+    });
+    __syncthreads();
+    auto settle = [&](bool exactly) {
+        const bool some = threadIdx.x < sm.n;
+        const u64 place = some ? sm.list[threadIdx.x] : 0;
+        const bool active = some && (exactly || weigh.bucket(logit_of(place)) == b);
+        narrow(sm, place, active ? weigh.weight(logit_of(place)) : 0, active, rank, before, border,
+               [&](u64 p) { return weigh.exact(logit_of(p)); });
+    };
+    const bool whole = sm.n <= LIST;
+    const int n_whole = whole ? (int)sm.n : -1;
+    while (!whole) {
         __syncthreads();
         if (threadIdx.x == 0) {
             sm.n = 0;
@@ -701,13 +727,8 @@ __device__ __forceinline__ int find_cut(const Row<BF16> &row, Shared &sm, const 
         lo = sm.lo;
         hi = sm.hi;
         const u64 none = ((u64)hi + 1) << 32;    // a cut above all of these (not above what was above them)
-        if (n <= LIST) {
-            const bool active = threadIdx.x < n;
-            const u64 place = active ? sm.list[threadIdx.x] : 0;
-            narrow(sm, place, active ? weigh.weight(logit_of(place)) : 0, active, rank, before, border,
-                   [&](u64 p) { return weigh.exact(logit_of(p)); });
-            return whole ? (int)n : -1;
-        }
+        if (n <= LIST)
+            break;
         if (lo == hi) {
             // ties: the first so many by index.  A thread takes chunks that follow one
             // another
@@ -791,6 +812,8 @@ __device__ __forceinline__ int find_cut(const Row<BF16> &row, Shared &sm, const 
         hi = hi - part * step;
         lo = below < step ? lo : hi - step + 1;
     }
+    settle(!whole);
+    return n_whole;
 }
 
 // `u` of a sum of weights, such that the token is the first whose sum is more
@@ -987,7 +1010,8 @@ __device__ __forceinline__ void choose_token(const SampleArgs &a, const Wish &wi
                     atomicAdd(&sm.slice[i], sum);
             }
             if (listed >= 0) {
-                if ((int)threadIdx.x < listed && sm.list[threadIdx.x] >= cut) {
+                if ((int)threadIdx.x < listed && sm.list[threadIdx.x] >= cut &&
+                    weigh.bucket(logit_of(sm.list[threadIdx.x])) == at) {
                     const u64 place = sm.list[threadIdx.x];
                     atomicAdd(&sm.slice[even_part_of(row.chunks, S, (index_of(place) + row.off) / Row<BF16>::EPC)],
                               weigh.weight(logit_of(place)));
