@@ -401,181 +401,181 @@ __global__ __launch_bounds__(NT, 2) void gemm_mx_kernel(MxArgs<CBF16> args)
     const uint32_t part = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / NXCD;
     const uint32_t all = (a.K + TK - 1) / TK;
     Share share = share_of(a.n_tiles, all, a.parts, part);
-  for (;;) {
-    const int t = share.unit, lo = share.at, n_kt = min(share.left, all - share.at);
-    const int grp = t / (GROUP_M * a.tiles_n), w = t % (GROUP_M * a.tiles_n);
-    const int rows = min((a.M + TM - 1) / TM - grp * GROUP_M, GROUP_M);
-    const int m0 = (grp * GROUP_M + w % rows) * TM, n0 = w / rows * TN;
+    for (;;) {
+        const int t = share.unit, lo = share.at, n_kt = min(share.left, all - share.at);
+        const int grp = t / (GROUP_M * a.tiles_n), w = t % (GROUP_M * a.tiles_n);
+        const int rows = min((a.M + TM - 1) / TM - grp * GROUP_M, GROUP_M);
+        const int m0 = (grp * GROUP_M + w % rows) * TM, n0 = w / rows * TN;
 
-    // Where this thread's chunks come from (rows past the last are the last; in a last
-    // stage, chunks past K are the last: those are cleared in the operands)
-    const int mr = min(TM, a.M - m0), nr = min(TN, a.N - n0);
-    const u32x4s ra = tileattn_dma::buffer_rsrc(a.A + (size_t)m0 * a.K, (uint32_t)mr * a.K * 2);
-    const u32x4s rw = tileattn_dma::buffer_rsrc(a.W + (size_t)n0 * (a.K / 2), (uint32_t)nr * (a.K / 2));
-    const u32x4s rs = tileattn_dma::buffer_rsrc(a.S + (size_t)n0 * (a.K / 32), (uint32_t)nr * (a.K / 32));
-    // A: slot s is row s / 16, stored chunk s % 16; W: row s / 4, stored chunk s % 4; scales:
-    // row s / 4, group s % 4
-    auto a_row = [&](int i) { return (i * NT + tid) / 16; };
-    auto a_ch = [&](int i) { return (tid % 16) ^ (a_row(i) & 15); };
-    const int w_ch = (tid % 4) ^ ((tid / 8) & 3), s_grp = tid % 4;   // (row / 2 % 4, for all its rows)
-    uint32_t ao[A_DMA];
-#pragma unroll
-    for (int i = 0; i < A_DMA; ++i)
-        ao[i] = (uint32_t)min(a_row(i), mr - 1) * a.K * 2;
-    uint32_t wr[T::W_DMA];
-#pragma unroll
-    for (int i = 0; i < T::W_DMA; ++i)
-        wr[i] = (uint32_t)min((i * NT + tid) / 4, nr - 1) * (a.K / 32);
-    auto dma = [&](int kt, unsigned char *to) {
-        const int k0 = (lo + kt) * TK, left = a.K - k0;
-        const uint32_t base = tileattn_dma::lds_addr(to);
-        int ac[A_DMA], wc = w_ch, sg = s_grp;
+        // Where this thread's chunks come from (rows past the last are the last; in a last
+        // stage, chunks past K are the last: those are cleared in the operands)
+        const int mr = min(TM, a.M - m0), nr = min(TN, a.N - n0);
+        const u32x4s ra = tileattn_dma::buffer_rsrc(a.A + (size_t)m0 * a.K, (uint32_t)mr * a.K * 2);
+        const u32x4s rw = tileattn_dma::buffer_rsrc(a.W + (size_t)n0 * (a.K / 2), (uint32_t)nr * (a.K / 2));
+        const u32x4s rs = tileattn_dma::buffer_rsrc(a.S + (size_t)n0 * (a.K / 32), (uint32_t)nr * (a.K / 32));
+        // A: slot s is row s / 16, stored chunk s % 16; W: row s / 4, stored chunk s % 4; scales:
+        // row s / 4, group s % 4
+        auto a_row = [&](int i) { return (i * NT + tid) / 16; };
+        auto a_ch = [&](int i) { return (tid % 16) ^ (a_row(i) & 15); };
+        const int w_ch = (tid % 4) ^ ((tid / 8) & 3), s_grp = tid % 4;   // (row / 2 % 4, for all its rows)
+        uint32_t ao[A_DMA];
 #pragma unroll
         for (int i = 0; i < A_DMA; ++i)
-            ac[i] = a_ch(i);
-        if (left < TK) {
+            ao[i] = (uint32_t)min(a_row(i), mr - 1) * a.K * 2;
+        uint32_t wr[T::W_DMA];
+#pragma unroll
+        for (int i = 0; i < T::W_DMA; ++i)
+            wr[i] = (uint32_t)min((i * NT + tid) / 4, nr - 1) * (a.K / 32);
+        auto dma = [&](int kt, unsigned char *to) {
+            const int k0 = (lo + kt) * TK, left = a.K - k0;
+            const uint32_t base = tileattn_dma::lds_addr(to);
+            int ac[A_DMA], wc = w_ch, sg = s_grp;
 #pragma unroll
             for (int i = 0; i < A_DMA; ++i)
-                ac[i] = min(ac[i], left / 8 - 1);
-            wc = min(wc, left / 32 - 1);
-            sg = min(sg, left / 32 - 1);
-        }
+                ac[i] = a_ch(i);
+            if (left < TK) {
 #pragma unroll
-        for (int i = 0; i < A_DMA; ++i)
-            tileattn_dma::dma16_soff(base + (i * NT + wave * 64) * 16, ao[i] + 16 * ac[i], k0 * 2, ra);
-#pragma unroll
-        for (int i = 0; i < T::W_DMA; ++i)
-            tileattn_dma::dma16_soff(base + A_STAGE + (i * NT + wave * 64) * 16, 16 * wr[i] + 16 * wc, k0 / 2, rw);
-#pragma unroll
-        for (int i = 0; i < T::W_DMA; ++i)
-            dma_byte(base + A_STAGE + W_STAGE + (i * NT + wave * 64) * 4, wr[i] + sg, k0 / 32, rs);
-    };
-
-    f32x16 acc[2][FN];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                acc[i][j][r] = 0.f;
-
-    // `part`: a last stage of less than 128, in which this lane's 32 of K may be past the
-    // end (`in`: they are not)
-    auto compute = [&](const unsigned char *st, auto part, bool in) {
-        u32x4 wv[FN];
-        float sc[FN];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int n = wn + 32 * j + col, q = 2 * kg + half;
-            wv[j] = *(const u32x4 *)(st + A_STAGE + n * 64 + 16 * (q ^ ((n >> 1) & 3)));
-            sc[j] = tileattn_mx::scale_of(*(const uint32_t *)(st + A_STAGE + W_STAGE + 4 * (n * 4 + q)));
-            if (part && !in) {
-                wv[j] = u32x4{0, 0, 0, 0};
-                sc[j] = 1.f;
+                for (int i = 0; i < A_DMA; ++i)
+                    ac[i] = min(ac[i], left / 8 - 1);
+                wc = min(wc, left / 32 - 1);
+                sg = min(sg, left / 32 - 1);
             }
-        }
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            bf16x8 av[2];
+            for (int i = 0; i < A_DMA; ++i)
+                tileattn_dma::dma16_soff(base + (i * NT + wave * 64) * 16, ao[i] + 16 * ac[i], k0 * 2, ra);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = wm + 32 * i + col, ch = 8 * kg + 4 * half + kk;
-                u32x4 x = *(const u32x4 *)(st + r * 256 + 16 * (ch ^ (r & 15)));
-                if (part && !in)
-                    x = u32x4{0, 0, 0, 0};
-                av[i] = __builtin_bit_cast(bf16x8, x);
-            }
+            for (int i = 0; i < T::W_DMA; ++i)
+                tileattn_dma::dma16_soff(base + A_STAGE + (i * NT + wave * 64) * 16, 16 * wr[i] + 16 * wc, k0 / 2, rw);
+#pragma unroll
+            for (int i = 0; i < T::W_DMA; ++i)
+                dma_byte(base + A_STAGE + W_STAGE + (i * NT + wave * 64) * 4, wr[i] + sg, k0 / 32, rs);
+        };
+
+        f32x16 acc[2][FN];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    acc[i][j][r] = 0.f;
+
+        // `part`: a last stage of less than 128, in which this lane's 32 of K may be past the
+        // end (`in`: they are not)
+        auto compute = [&](const unsigned char *st, auto part, bool in) {
+            u32x4 wv[FN];
+            float sc[FN];
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const bf16x8 wb = tileattn_mx::eight(wv[j][kk], sc[j]);
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    acc[i][j] = mfma(wb, av[i], acc[i][j]);
+                const int n = wn + 32 * j + col, q = 2 * kg + half;
+                wv[j] = *(const u32x4 *)(st + A_STAGE + n * 64 + 16 * (q ^ ((n >> 1) & 3)));
+                sc[j] = tileattn_mx::scale_of(*(const uint32_t *)(st + A_STAGE + W_STAGE + 4 * (n * 4 + q)));
+                if (part && !in) {
+                    wv[j] = u32x4{0, 0, 0, 0};
+                    sc[j] = 1.f;
+                }
             }
-        }
-    };
-
-    // stage kt lives in kt % TST; the loads of up to TST - 2 later ones may stay in flight
-    // at its beginning, and the barrier frees the stage before it
-    const int n_whole = n_kt - ((lo + n_kt) * TK > a.K);
 #pragma unroll
-    for (int s = 0; s < TST - 1; ++s)
-        if (s < n_kt)
-            dma(s, lds + s * STAGE);
-    for (int kt = 0; kt < n_whole; ++kt) {
-        if (kt + 1 < n_kt)
-            tileattn_dma::wait_vmcnt<T::DMAS * (TST - 2)>();
-        else
+            for (int kk = 0; kk < 4; ++kk) {
+                bf16x8 av[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = wm + 32 * i + col, ch = 8 * kg + 4 * half + kk;
+                    u32x4 x = *(const u32x4 *)(st + r * 256 + 16 * (ch ^ (r & 15)));
+                    if (part && !in)
+                        x = u32x4{0, 0, 0, 0};
+                    av[i] = __builtin_bit_cast(bf16x8, x);
+                }
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const bf16x8 wb = tileattn_mx::eight(wv[j][kk], sc[j]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        acc[i][j] = mfma(wb, av[i], acc[i][j]);
+                }
+            }
+        };
+
+        // stage kt lives in kt % TST; the loads of up to TST - 2 later ones may stay in flight
+        // at its beginning, and the barrier frees the stage before it
+        const int n_whole = n_kt - ((lo + n_kt) * TK > a.K);
+#pragma unroll
+        for (int s = 0; s < TST - 1; ++s)
+            if (s < n_kt)
+                dma(s, lds + s * STAGE);
+        for (int kt = 0; kt < n_whole; ++kt) {
+            if (kt + 1 < n_kt)
+                tileattn_dma::wait_vmcnt<T::DMAS * (TST - 2)>();
+            else
+                tileattn_dma::wait_vmcnt<0>();
+            __syncthreads();
+            const int nx = kt + TST - 1;
+            if (nx < n_kt)
+                dma(nx, lds + nx % TST * STAGE);
+            compute(lds + kt % TST * STAGE, std::false_type{}, true);
+        }
+        if (n_whole < n_kt) {
             tileattn_dma::wait_vmcnt<0>();
-        __syncthreads();
-        const int nx = kt + TST - 1;
-        if (nx < n_kt)
-            dma(nx, lds + nx % TST * STAGE);
-        compute(lds + kt % TST * STAGE, std::false_type{}, true);
-    }
-    if (n_whole < n_kt) {
-        tileattn_dma::wait_vmcnt<0>();
-        __syncthreads();
-        compute(lds + n_whole % TST * STAGE, std::true_type{}, (lo + n_whole) * TK + 64 * kg + 32 * half < a.K);
-    }
-
-    // The two groups' sums meet in LDS, row by row of C; then all waves store, whole lines.
-    // Lane: row wm + 32 i + col, columns wn + 32 j + 8 q + 4 half .. + 3; 16-byte chunk c of
-    // row r at c ^ (r % 32).
-    float *const sums = (float *)lds;
-    auto at = [&](int r, int c) { return (f32x4 *)(sums + r * TN + 4 * (c ^ (r & 31))); };
-    __syncthreads();
-    if (kg == 1)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *at(wm + 32 * i + col, (wn + 32 * j) / 4 + 2 * q + half) =
-                        f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    __syncthreads();
-    if (kg == 0)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *at(wm + 32 * i + col, (wn + 32 * j) / 4 + 2 * q + half) +=
-                        f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    __syncthreads();
-    constexpr int U = 4, RPI = NT / (TN / 4);        // rows at a time, U steps of them
-    const int c = tid % (TN / 4), n = n0 + 4 * c, r0 = tid / (TN / 4);
-    if ((uint32_t)n_kt == all) {
-        typename EArgs<CBF16>::template Added<U> now, next;
-        now.load(a, m0 + r0, RPI, n);
-#pragma unroll 1
-        for (int r = r0; r < TM; r += U * RPI) {
-            f32x4 x[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                x[u] = *at(r + u * RPI, c);
-            if (r + U * RPI < TM)
-                next.load(a, m0 + r + U * RPI, RPI, n);
-            a.store(m0 + r, RPI, n, x, now);
-            now = next;
+            __syncthreads();
+            compute(lds + n_whole % TST * STAGE, std::true_type{}, (lo + n_whole) * TK + 64 * kg + 32 * half < a.K);
         }
-    } else {
-        float *const rec = (float *)a.C + (2 * (size_t)part + (lo == 0)) * TM * TN;
+
+        // The two groups' sums meet in LDS, row by row of C; then all waves store, whole lines.
+        // Lane: row wm + 32 i + col, columns wn + 32 j + 8 q + 4 half .. + 3; 16-byte chunk c of
+        // row r at c ^ (r % 32).
+        float *const sums = (float *)lds;
+        auto at = [&](int r, int c) { return (f32x4 *)(sums + r * TN + 4 * (c ^ (r & 31))); };
+        __syncthreads();
+        if (kg == 1)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *at(wm + 32 * i + col, (wn + 32 * j) / 4 + 2 * q + half) =
+                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __syncthreads();
+        if (kg == 0)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *at(wm + 32 * i + col, (wn + 32 * j) / 4 + 2 * q + half) +=
+                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __syncthreads();
+        constexpr int U = 4, RPI = NT / (TN / 4);        // rows at a time, U steps of them
+        const int c = tid % (TN / 4), n = n0 + 4 * c, r0 = tid / (TN / 4);
+        if ((uint32_t)n_kt == all) {
+            typename EArgs<CBF16>::template Added<U> now, next;
+            now.load(a, m0 + r0, RPI, n);
+#pragma unroll 1
+            for (int r = r0; r < TM; r += U * RPI) {
+                f32x4 x[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    x[u] = *at(r + u * RPI, c);
+                if (r + U * RPI < TM)
+                    next.load(a, m0 + r + U * RPI, RPI, n);
+                a.store(m0 + r, RPI, n, x, now);
+                now = next;
+            }
+        } else {
+            float *const rec = (float *)a.C + (2 * (size_t)part + (lo == 0)) * TM * TN;
 #pragma unroll 4
-        for (int r = r0; r < TM; r += RPI)
-            *(f32x4 *)(rec + r * TN + 4 * c) = *at(r, c);
+            for (int r = r0; r < TM; r += RPI)
+                *(f32x4 *)(rec + r * TN + 4 * c) = *at(r, c);
+        }
+        share.left -= n_kt;
+        if (share.left == 0)
+            return;
+        ++share.unit;
+        share.at = 0;
+        tileattn_dma::wait_vmcnt<0>();   // (the stores: the next tile's loads are counted by hand)
+        __syncthreads();                 // the sums have been read
     }
-    share.left -= n_kt;
-    if (share.left == 0)
-        return;
-    ++share.unit;
-    share.at = 0;
-    tileattn_dma::wait_vmcnt<0>();   // (the stores: the next tile's loads are counted by hand)
-    __syncthreads();                 // the sums have been read
-  }
 }
 
 // The partial sums of the strips (of `width` columns, all rows) or tiles that were cut,

@@ -22,7 +22,7 @@
 //
 // Measured: 256 x 131072 bf16 with every filter 40 us (the row's way to registers 10, where
 // HBM's floor is 11 for all; the largest 2, exponentials of all logits 4, the rest barriers and
-// LDS); 64 x 128001 fp32 by top-p 76 (14, 14 and 47 for the three kernels: the last one's
+// LDS); 64 x 128001 fp32 by top-p 70 (14, 14 and 41 for the three kernels: the last one's
 // passes over a row by one workgroup); 1 x 32000 18.  Tried: the candidates sorted in LDS
 // (55 steps of a bitonic network of 1024, 0.3 us each), compared each with each up to 1024
 // (30 us for 500), the workgroup's sums by shuffles through LDS (a place took 8 us instead of
