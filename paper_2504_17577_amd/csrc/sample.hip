@@ -872,7 +872,7 @@ __device__ __forceinline__ void choose_token(const SampleArgs &a, const Wish &wi
                 n += ns;
             }
         }
-        auto exact = [&](u64 p) { return exp((double)(logit_of(p) - best) * weigh.inv_T) * UNIT; };
+        auto exact = [&](u64 p) { return exp(((double)logit_of(p) - (double)best) * weigh.inv_T) * UNIT; };
         const u64 w = active ? (u64)(exact(place) + 0.5) : 0;
         // by top-k alone, for the weight that top_p is a part of (of no account without it); then by all
         Border border = {(u64)wish.k, INFINITY, 0.0};
