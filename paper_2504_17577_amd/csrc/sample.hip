@@ -448,7 +448,8 @@ __device__ __forceinline__ Slice find_candidates(const SampleArgs &a, const Wish
 
     // the border: the first of SUBS steps down to the lowest of the groups' largest that
     // has k of them above it; if there are not k, whatever is not -inf
-    const float range = m - low, step = range > 0.f && range < INFINITY ? (SUBS - 1) / range : 0.f;
+    // (groups so close, or so far apart, that fp32 has no such steps: one step, which all are in)
+    const float range = m - low, steps = (SUBS - 1) / range, step = range < INFINITY && steps < INFINITY ? steps : 0.f;
     auto level = [&](float x) { return (m - x) * step; };
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i)
