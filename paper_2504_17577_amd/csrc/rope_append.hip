@@ -52,6 +52,33 @@ __device__ __forceinline__ float from_lane(float x, int l) { return __shfl(x, l,
 template <int HL>
 __device__ __forceinline__ double from_lane(double x, int l) { return __shfl(x, l, HL); }
 
+// 1 / sqrt(mean(x^2) + eps) where 32 bits do not hold the sum or squares that count in it:
+// of x over a power of two, the larger one of x's and of the root of eps
+template <int HL>
+__device__ __forceinline__ float norm_far(float (&x)[8], float eps)
+{
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        top = fmaxf(top, fabsf(x[i]));
+#pragma unroll
+    for (int m = 1; m < HL; m *= 2)
+        top = fmaxf(top, __shfl_xor(top, m, HL));
+    int e = __builtin_amdgcn_frexp_expf(top);
+    if (eps > 0.f)
+        e = max(e, (__builtin_amdgcn_frexp_expf(eps) + 1) / 2);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] = ldexpf(x[i], -e);
+        sum += x[i] * x[i];
+    }
+#pragma unroll
+    for (int m = 1; m < HL; m *= 2)
+        sum += __shfl_xor(sum, m, HL);
+    return 1.f / sqrtf(sum * (1.f / (8 * HL)) + ldexpf(eps, -2 * e));
+}
+
 // One head's eight numbers of this lane, normed (with a weight) and rotated: F is the
 // arithmetic's type.  Pairs of halves: the partner's numbers are those of the lane
 // rot / 16 to the right or left; pairs of neighbours: the lane's own.
@@ -67,7 +94,11 @@ __device__ __forceinline__ void normed_rotated(const RopeArgs &a, int ch, const 
 #pragma unroll
         for (int m = 1; m < HL; m *= 2)
             sum += __shfl_xor(sum, m, HL);
-        const F r = F(1) / sqrt(sum * F(1.0 / (8 * HL)) + F(a.eps));
+        const F mean = sum * F(1.0 / (8 * HL)) + F(a.eps);
+        F r = F(1) / sqrt(mean);
+        if constexpr (sizeof(F) == 4)
+            if (!(mean >= 0x1p-100f && mean < INFINITY))   // (the same for all of a head's lanes)
+                r = norm_far<HL>(x, a.eps);
         const u32x4 wv = *(const u32x4 *)(w + 8 * ch);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
