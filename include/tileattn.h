@@ -714,9 +714,9 @@ ta_status gemm_mxfp4_plan(int M, int N, int K, int *num_parts);
  *   logp    device, fp32 [B]                                               written
  *   1 <= B <= 65536, 1 <= V <= 2^20 (else TA_ERR_INVALID_SHAPE); token and logp apart from
  *   each other and every input (TA_ERR_ALIASING)
- *   workspace  device, 16-byte aligned, at least sample_workspace_bytes(...) bytes, owned
- *           by the caller, its contents on entry of no account, no overlap with any other
- *           argument; TA_ERR_WORKSPACE if NULL or smaller
+ *   workspace  device, 16-byte aligned, at least sample_logits_workspace_bytes(...) bytes,
+ *           owned by the caller, its contents on entry of no account, no overlap with any
+ *           other argument; TA_ERR_WORKSPACE if NULL or smaller
  *
  * A logit of -inf is never chosen.  A row with NaN or +inf in it, or with -inf only, has
  * token -1 and logp NaN.  Weights are computed in fp64 and added exactly, as whole
@@ -729,7 +729,12 @@ ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const fl
                         const float *min_p, int *token, float *logp, int B, int V,
                         void *workspace, size_t workspace_bytes, void *stream);
 
-/* Workspace bytes sample_logits needs (0 for short rows and for many).  No HIP call. */
+/* Workspace bytes sample_logits needs for logits of one type (0 where one workgroup takes a
+ * row: of up to 32768 logits or, from 128 rows on, up to 69627 in fp32 and 139255 in bf16).
+ * No HIP call. */
+ta_status sample_logits_workspace_bytes(int B, int V, int l_bf16, size_t *bytes);
+
+/* The same for either type: fp32's, bf16 needs no more.  No HIP call. */
 ta_status sample_workspace_bytes(int B, int V, size_t *bytes);
 
 /*

@@ -1128,8 +1128,9 @@ __global__ __launch_bounds__(NT) void sample_choose_kernel(SampleArgs a)
 // Slices of a row: one workgroup takes rows of up to 32768 logits, and any where there
 // are rows for half of the CUs; a slice has HELD NT chunks of 16 bytes at most (a row
 // touches up to two more than it has bytes for)
-int slices_of(int B, int V, int per_chunk = 4)
+int slices_of(int B, int V, int l_bf16)
 {
+    const int per_chunk = l_bf16 ? 8 : 4;
     const int least = (V / per_chunk + 2 + HELD * NT - 1) / (HELD * NT);
     if (V <= 32768 || B >= 128)
         return least;
@@ -1140,11 +1141,11 @@ struct Workspace {
     size_t slices, lists, weights, counts, all;
 };
 
-Workspace workspace_of(int B, int V)
+Workspace workspace_of(int B, int slices)
 {
-    const size_t n = (size_t)B * slices_of(B, V);
+    const size_t n = (size_t)B * slices;
     Workspace w = {};
-    if (slices_of(B, V) == 1)
+    if (slices == 1)
         return w;
     w.lists = w.slices + (n * sizeof(Slice) + 15) / 16 * 16;
     w.weights = w.lists + (size_t)B * LIST * 8;
@@ -1185,7 +1186,8 @@ ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const fl
     for (const Span &s : in)
         if (overlaps(out[0], s) || overlaps(out[1], s))
             return TA_ERR_ALIASING;
-    const Workspace w = workspace_of(B, V);        // (enough for either type)
+    const int slices = slices_of(B, V, l_bf16);
+    const Workspace w = workspace_of(B, slices);
     if (w.all) {
         if (!workspace || workspace_bytes < w.all)
             return TA_ERR_WORKSPACE;
@@ -1199,7 +1201,7 @@ ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const fl
                 return TA_ERR_ALIASING;
     }
     unsigned char *const ws = (unsigned char *)workspace;
-    const SampleArgs a = {logits, stride, u, temperature, top_k, top_p, min_p, token, logp, V, slices_of(B, V, l_bf16 ? 8 : 4),
+    const SampleArgs a = {logits, stride, u, temperature, top_k, top_p, min_p, token, logp, V, slices,
                           (Slice *)(ws + w.slices), (u64 *)(ws + w.lists), (u64 *)(ws + w.weights),
                           (uint32_t *)(ws + w.counts)};
     hipStream_t s = (hipStream_t)stream;
@@ -1220,15 +1222,18 @@ ta_status sample_logits(const void *logits, int64_t stride, int l_bf16, const fl
     return e == hipSuccess ? TA_OK : TA_ERR_LAUNCH;
 }
 
-ta_status sample_workspace_bytes(int B, int V, size_t *bytes)
+ta_status sample_logits_workspace_bytes(int B, int V, int l_bf16, size_t *bytes)
 {
     if (!bytes)
         return TA_ERR_NULL_POINTER;
     const ta_status rc = check_sample_sizes(B, V);
     if (rc != TA_OK)
         return rc;
-    *bytes = workspace_of(B, V).all;
+    *bytes = workspace_of(B, slices_of(B, V, l_bf16)).all;
     return TA_OK;
 }
+
+// (fp32's rows have as many slices as bf16's, or more)
+ta_status sample_workspace_bytes(int B, int V, size_t *bytes) { return sample_logits_workspace_bytes(B, V, 0, bytes); }
 
 }  // extern "C"

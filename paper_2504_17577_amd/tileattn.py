@@ -138,6 +138,8 @@ def lib():
     L.gemm_mxfp4_plan.argtypes = [i, i, i, ctypes.POINTER(i)]
     L.sample_logits.restype = i
     L.sample_logits.argtypes = [p, ctypes.c_int64, i] + [p] * 7 + [i, i, p, ctypes.c_size_t, p]
+    L.sample_logits_workspace_bytes.restype = i
+    L.sample_logits_workspace_bytes.argtypes = [i, i, i, ctypes.POINTER(ctypes.c_size_t)]
     L.sample_workspace_bytes.restype = i
     L.sample_workspace_bytes.argtypes = [i, i, ctypes.POINTER(ctypes.c_size_t)]
     L.ta_schedule.restype = i
@@ -1116,9 +1118,13 @@ def gemm_mxfp4_epilogue(a, w, w_scale, bias=None, activation: str = "none", resi
 
 
 @functools.lru_cache(maxsize=4096)
-def sample_workspace_bytes(B: int, V: int) -> int:
+def sample_workspace_bytes(B: int, V: int, dtype=None) -> int:
+    """For logits of ``dtype`` or (None) either type."""
     n = ctypes.c_size_t()
-    rc = lib().sample_workspace_bytes(B, V, ctypes.byref(n))
+    if dtype is None:
+        rc = lib().sample_workspace_bytes(B, V, ctypes.byref(n))
+    else:
+        rc = lib().sample_logits_workspace_bytes(B, V, int(dtype == torch.bfloat16), ctypes.byref(n))
     if rc != TA_OK:
         raise TileAttnError(rc, ta_status_string(rc))
     return n.value
@@ -1135,8 +1141,8 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     fewest that hold top_p of their weight, and those of min_p times the largest weight or
     more; u picks one by the stayed weights' sums in the order of indexes.  A row without a
     finite largest logit, or with NaN in it, gets token -1 and logp NaN.  ``workspace``, a
-    uint8 GPU tensor of at least sample_workspace_bytes(B, V) bytes, is allocated here if
-    needed and not given."""
+    uint8 GPU tensor of at least sample_workspace_bytes(B, V, logits.dtype) bytes, is
+    allocated here if needed and not given."""
     if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or not logits.is_cuda:
         raise TypeError("logits must be a 2-D float32 or bfloat16 GPU tensor [B, V]")
     B, V = logits.shape
@@ -1150,7 +1156,7 @@ def sample_logits(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
             _vector(name, t, dtype, (B,))
     token = _output("token", token, (B,), torch.int32, logits)
     logp = _output("logp", logp, (B,), torch.float32, logits)
-    need = sample_workspace_bytes(B, V)
+    need = sample_workspace_bytes(B, V, logits.dtype)
     if workspace is None:
         if need:
             workspace = _workspace(need, logits, stream)
