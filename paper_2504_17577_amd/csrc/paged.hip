@@ -5,8 +5,6 @@
 #include <math.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "cache_checks.h"
 #include "mxfp4.h"
 #include "paged_plan.h"
@@ -430,9 +428,17 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
             if (steps > 1)
                 lookup(1);
         }
-        // `tail`: whether there are keys past the last in the step (uniform)
-        auto step = [&](int s, auto tail) {
+        // `tail`: whether there are keys past the last in the step (uniform); `more`: whether others
+        // follow.  Of 4 bits the last step by itself: the masks in every step, for the last one's
+        // sake, were a sixth of the vector instructions.  (Loops around the body; as a function of
+        // the step it took up to 8 registers more, with 64 dims of 16 bits and 17 to 32 heads a third
+        // of the waves: 1024 sequences mixed to 300, 20 query heads to each of 4 K/V heads, 64 us
+        // instead of 52.)
+#pragma unroll
+        for (int part = MX ? 0 : 1; part < 2; ++part)
+        for (int s = MX && part ? max(steps - 1, 0) : 0; s < (part ? steps : steps - 1); ++s) {
             const int key0 = first + s * KS;
+            const bool tail = MX ? part == 1 : key0 + KS > k_hi, more = MX ? part == 0 : s + 1 < steps;
             // The K loads took whole lines of eight rows each (halves of sixteen rows'
             // lines would come from HBM twice); lanes c16 and c16 ^ 8 exchange what the
             // other's row needs: then lane c16 holds chunks 8 l + g and 8 l + 4 + g of row c16
@@ -473,7 +479,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
                 bad[kb] = next_bad[kb];
-            if (s + 1 < steps) {
+            if (more) {
                 place(s + 1);
                 load_k();
                 if (s + 2 < steps)
@@ -605,19 +611,10 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_paged_kernel(PagedArgs a)
                         }
                 }
             }
-            if (s + 1 < steps)
+            if (more)
                 load_v();
-        };
-        if constexpr (MX) {
-            // the last step by itself: the masks in every step, for the last one's sake, were a
-            // sixth of the vector instructions
-            for (int s = 0; s + 1 < steps; ++s)
-                step(s, std::false_type{});
-            if (steps > 0)
-                step(steps - 1, std::true_type{});
-        } else {
-            for (int s = 0; s < steps; ++s)
-                step(s, first + (s + 1) * KS > k_hi);
+            if (MX && part)
+                break;
         }
 
         // The waves' sums meet in LDS, in wave order.  Lane: row c16, dims
