@@ -985,13 +985,22 @@ ta_status attn_paged_plan(int B, int Hq, int Hkv, int D, int page_size, int max_
 }
 
 // The keys of a cache in 4 bits cost more of the vector ALU's time than of HBM's: three
-// workgroups on a CU hide each other's loads better than two.  us, 512 | 768 | 1024 parts:
-// 64 sequences mixed to 16384 44.0 | 40.4 | 43.3, one of 100001 32.2 | 31.6 | 35.1, 32 mixed to
-// 4000 with 32 K/V heads of 64 dims 29.6 | 25.7 | 25.3
+// workgroups on a CU hide each other's loads better than two.  More than 16 query heads to a
+// workgroup take registers and LDS of which, with 128 dims, a CU has for two (768 parts would run
+// in one and a half rounds), and their partial results are larger.  us, 512 | 768 | 1024 parts,
+// 128 dims, then 64:
+//   64 mixed to 16384, 32 heads on 8     130|127|127    88.2|87.2|87.4
+//   32 mixed to 4000, 32 on 32           69.6|60.4|63.6 50.9|45.2|44.6
+//   one of 100001, 32 on 8               30.8|31.4|35.1 24.9|25.0|25.9
+//   8 of 16384, 64 on 4                  19.7|21.2|24.7 16.1|17.5|17.6
+//   64 mixed to 16384, 80 on 4           102|109|111    65.5|61.9|64.2
+//   64 mixed to 8192, 64 on 2            41.2|46.5|47.2 27.3|27.6|31.7
+//   16 mixed to 4096, 136 on 8           25.4|30.7|32.0 19.9|20.8|23.1
+//   one of 100001, 64 on 1               26.9|33.8|39.8 23.1|27.3|33.0
 ta_status attn_paged_mxfp4_plan(int B, int Hq, int Hkv, int D, int page_size, int max_pages, int *num_parts)
 {
     const ta_status rc = attn_paged_plan(B, Hq, Hkv, D, page_size, max_pages, num_parts);
-    if (rc == TA_OK && *num_parts)
+    if (rc == TA_OK && *num_parts && paged_block_rows(Hq / Hkv) <= 16)
         *num_parts = 768;
     return rc;
 }
