@@ -87,6 +87,8 @@ __device__ __forceinline__ void normed_rotated(const RopeArgs &a, int ch, const 
                                                const float (&sn)[8], F (&x)[8])
 {
     if (w) {
+        // (loaded here: behind the branch below it made 16384 tokens' 72 us 73.2, in 4 bits 96 us 101)
+        const u32x4 wv = *(const u32x4 *)(w + 8 * ch);
         F sum = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -99,7 +101,6 @@ __device__ __forceinline__ void normed_rotated(const RopeArgs &a, int ch, const 
         if constexpr (sizeof(F) == 4)
             if (!(mean >= 0x1p-100f && mean < INFINITY))   // (the same for all of a head's lanes)
                 r = norm_far<HL>(x, a.eps);
-        const u32x4 wv = *(const u32x4 *)(w + 8 * ch);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] = x[2 * i] * r * F(bf16_lo(wv[i]));
