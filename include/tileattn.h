@@ -551,7 +551,8 @@ typedef enum {
  * cache has no place for has its queries all the same.
  *
  * Queries, and keys for a bf16 cache, are computed in fp32 and rounded once, to nearest
- * even.  Keys for 8 and 4 bits are computed in fp64, rounded to fp32 and then to the
+ * even (the norm over all of bf16's range, whatever fp32 makes of its squares).  Keys for
+ * 8 and 4 bits are computed in fp64, rounded to fp32 and then to the
  * cache's type; e4m3 as kv_cache_append does.  MXFP4: the scale is the power of two that
  * puts a group's largest number between 3.5 and 7 (at least 2^-126, at most 2^125), the
  * codes are the nearest (to even), beyond 6 as 6, infinities too; a NaN makes its

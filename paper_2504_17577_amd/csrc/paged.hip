@@ -254,7 +254,8 @@ __device__ __forceinline__ Place place_of(const PagedArgs &a, uint32_t HR, int c
 // makes pairs of neighbouring dims of a key into bf16, scale included, then pairs of keys by
 // byte permutes; the scales of a lane's four keys come from the four lanes that loaded them.
 // The vector ALU bounds it (about 140 instructions per 16 keys of a wave, half the time on
-// each SIMD) and the loads' way, which two or three waves on a SIMD do not hide: 64 sequences of up to 16384 mixed 34 us (3.7 TB/s), B=1 Sk=100001 25 us (4.3 TB/s).
+// each SIMD) and the loads' way, which two or three waves on a SIMD do not hide: 64 sequences
+// of up to 16384 mixed 34 us (3.7 TB/s), B=1 Sk=100001 25 us (4.3 TB/s).
 // Tried: 64 keys a step (195 registers, two workgroups a CU: 54 us and 35 with the merge
 // instead of 40 and 32), loads two steps ahead (217 registers: 46 and 33).
 template <int D, int TYPE, int RT>

@@ -135,10 +135,13 @@ __device__ __forceinline__ void normed_rotated(const RopeArgs &a, int ch, const 
 // Queries and what a bf16 cache takes are computed in 32 bits.  Keys for 8 and 4 bits
 // are computed in 64 and rounded to 32 bits once before they meet the cache's type: a
 // key next to the border of two of its numbers (a quarter of the value apart in 4 bits)
-// falls where the exact one does.  HBM bounds a prefill
-// (16384 tokens of 32 + 8 + 8 heads of 128 dims into bf16, 411 MB both ways: 72 us, 5.7 TB/s,
-// the rate of a copy), the loads one behind the other (seq and pos, the table, then the row)
-// a few tokens (32: 3.3 us; 2047 into 4 bits 14, of a floor of 9).
+// falls where the exact one does.  HBM bounds a prefill into bf16 (16384 tokens of 32 + 8 + 8
+// heads of 128 dims, normed, 411 MB read and written: 72 us, 5.7 TB/s; a copy of 2 GiB reaches
+// 4.8), the loads one behind the other (seq and pos, the table, then the row) a few tokens (32:
+// 3.2 us, 3.7 into 8 and 4 bits).  Keys in 64 bits take 94 registers, five waves a SIMD where bf16
+// has eight, and e4m3's a division by the scale each: 16384 tokens into 8 bits 108 us of 80 at the
+// copy's rate, 92 without the norm, into 4 bits 95 of 75, 78 without; 2047 tokens 12, 17.8 and
+// 15.7 us.  Keys and values alone (kv_cache_append into 4 bits): 16384 tokens 33 us of 18, 2047 6.1.
 template <int D, int TYPE, bool INTER>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeArgs a)
 {
@@ -306,7 +309,13 @@ ta_status qk_norm_rope_append(const void *Q, const void *K, const void *V, int64
                         (const uint16_t *)q_weight, (const uint16_t *)k_weight, cos_sin, seq, pos, (uint16_t *)Q_out,
                         K_cache, V_cache, k_scale, v_scale, page_table, eps, cos_sin ? rot_dim : 0, num_positions,
                         B, Hq, Hkv, num_pages, __builtin_ctz(page_size), max_pages};
-    const int rounds = (Hq + 2 * Hkv + 2048 / D - 1) / (2048 / D);   // of the heads that 256 threads take at a time
+    // Rounds of the heads that 256 threads take at a time: a workgroup each for few tokens, else one
+    // behind the other (a token's angles are loaded once).  us, three workgroups a token | one, 32 + 8 +
+    // 8 heads of 128 dims, normed, into bf16, 8 and 4 bits:
+    //   T = 32    3.2|4.8, 3.8|5.4, 3.6|5.3       512   5.8|6.7, 7.2|7.5, 6.7|7.1
+    //   1023      8.4|8.4, 11.4|9.9, 10.9|9.0     1536  10.8|10.3, 15.3|15.5, 14.6|13.8
+    //   2047      13.2|12.1, 19.3|17.8, 18.3|15.7 16384 84|73, 132|108, 126|95
+    const int rounds = (Hq + 2 * Hkv + 2048 / D - 1) / (2048 / D);
     const dim3 grid((unsigned)T, (unsigned)(T < 1024 ? rounds : 1));
     hipStream_t s = (hipStream_t)stream;
     const bool inter = interleaved != 0;

@@ -1127,7 +1127,21 @@ __global__ __launch_bounds__(NT) void sample_choose_kernel(SampleArgs a)
 
 // Slices of a row: one workgroup takes rows of up to 32768 logits, and any where there
 // are rows for half of the CUs; a slice has HELD NT chunks of 16 bytes at most (a row
-// touches up to two more than it has bytes for)
+// touches up to two more than it has bytes for).  Slices pay for the histogram's passes over a
+// row, candidates (a small top-k) cost two kernels more with them; the host does not know
+// which a row takes.  us, 1 | 2 | 4 slices | as many as here, top-k 40 with top-p | top-p alone:
+//   1 x 32768 fp32     18.1 22.1 26.8 | 18.1     35.0 34.5 31.8 | 35.0
+//   64 x 32768 fp32    19.7 23.8 27.7 | 19.7     37.1 38.4 37.0 | 37.1
+//   1 x 40000 fp32     19.5 22.8 27.0 | 26.7     40.3 37.8 34.5 | 34.1
+//   64 x 50000 fp32    23.0 25.5 29.5 | 36.7     52.9 49.6 45.5 | 50.6
+//   1 x 152064 bf16       - 28.9 30.2 | 55.3        - 78.9 59.4 | 52.8
+//   127 x 131072 bf16  32.4 32.2 41.5 | 41.3     105  81.9 73.2 | 73.7
+//   128 x 131072 bf16  32.3 32.0 41.7 | 32.0     105  82.3 73.8 | 105
+//   256 x 131072 bf16  37.2 47.0 62.5 | 37.5     113  103  98.3 | 113
+//   256 x 152064 bf16     - 51.3 66.8 | 51.5        - 116  109  | 117
+// (55.3: 18 slices allow no candidates for a top-k of 40.)  A longer HELD would take 152064
+// 16-bit logits in one slice too; candidates have its chunks in registers, of which 122 of
+// 128 are taken.
 int slices_of(int B, int V, int l_bf16)
 {
     const int per_chunk = l_bf16 ? 8 : 4;
