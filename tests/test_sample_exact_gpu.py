@@ -22,6 +22,11 @@ ROWS = [
     ((1.0409735, -0.9768613), 0.95, 0.13294299, None, 1),
     ((1.0, -0.75056094), 0.85202354, None, None, 1),
     ((1.0, -0.6177085), 0.83447886, None, None, 0),
+    # weights that are 1.5, 1.1 and 0.2 10^-14 of themselves above min_p: what the series of a
+    # histogram's weights may be off by
+    ((0.91615325, -3.5037196), 0.99, 0.012035763, None, 1),
+    ((3.5544543, -0.06282974), 0.98, 0.026855515, None, 1),
+    ((1.0400137, -0.5636859), 0.9, 0.20115097, None, 1),
 ]
 # (length the row is padded to with -inf, rows, top_k): how the kernels take it
 WAYS = [(2, 1, None), (2, 5, 2), (1000, 1, None), (1025, 1, None), (2000, 3, None), (2000, 3, 2), (32768, 1, None),
@@ -30,7 +35,7 @@ WAYS = [(2, 1, None), (2, 5, 2), (1000, 1, None), (1025, 1, None), (2000, 3, Non
 
 
 @pytest.mark.parametrize("V,B,k", WAYS, ids=str)
-@pytest.mark.parametrize("row", ROWS, ids=["min_p", "u above", "u below"])
+@pytest.mark.parametrize("row", ROWS, ids=["min_p", "u above", "u below", "1.5e-14", "1.1e-14", "2e-15"])
 def test_one_answer_whichever_way_a_row_takes(ta, row, V, B, k):  # noqa: F811
     few, u, m, p, want = row
     first = np.float32(few)
